@@ -9,6 +9,10 @@
  *                             this instance holds in its token-granular pool
  *   esp_merge_partials        log-sum-exp combination of partial results
  *   esp_kv_append             scatter of K/V rows into scheduler-chosen slots
+ *   esp_partial_attn_decode_shared  decode of requests that share a long prefix
+ *   esp_qk_norm_rope_append   norm and rotation of new queries and keys on their
+ *                             way to attention and into the pool
+ *   esp_extend_block_table, esp_build_slots  pages and slot lists from lengths
  * and, on the host, the scheduler's two numeric helpers for the prefill phase:
  *   esp_plan_prefill_batches  batching plan (dynamic program over requests and instances)
  *   esp_fit_prefill_model     least-squares fit of the iteration-time model
@@ -337,6 +341,115 @@ esp_status esp_partial_attn_prefill_pool_direct(
     int32_t Hq, int32_t Hkv, int32_t D, float softmax_scale, int32_t causal,
     int32_t out_f32, void* O, float* LSE,
     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Decode partial attention behind shared prefixes: requests that begin with the
+ * same tokens (a system prompt, a document that many questions are asked about)
+ * name the same pool rows for them, and those are read once for all of the
+ * requests and not once for each.  Requests come in groups of consecutive ones;
+ * request b of group g attends its single query token to the rows
+ *   prefix_slots[prefix_offsets[g] .. prefix_offsets[g+1])   and
+ *   slot_idx[seq_offsets[b] .. seq_offsets[b+1])
+ * (no mask).  The result is that of esp_partial_attn_decode on the two lists put
+ * together, up to the order of fp32 additions and one rounding of the weights.  Either list may be
+ * empty; a request that has neither gives O = 0, LSE = -inf.
+ *
+ *   group_offsets int32 [n_groups+1]: requests of group g, from 0 to B;
+ *   prefix_offsets int32 [n_groups+1], from 0 to prefix_total; prefix_slots int32 [prefix_total].
+ *   max_prefix, max_group: upper bounds of a prefix's tokens and of a group's
+ *     requests (host-known).  A request past max_group of its group is left
+ *     without the prefix.
+ *   Everything else as in esp_partial_attn_decode (max_len: of the requests' own
+ *   lists).  B = 0 writes nothing.  n_groups = 0 needs prefix_total = 0: the group arrays may
+ *   then be NULL.
+ *   workspace: at least esp_decode_shared_workspace_bytes(...) bytes, 256-byte
+ *   aligned; contents need not be preserved.  0 from there: the call would be refused.
+ * With esp_debug_set_validate the two lists and three offset arrays are checked as
+ * in esp_partial_attn_decode.
+ */
+esp_status esp_partial_attn_decode_shared(
+    const void* q, const void* k_pool, const void* v_pool, int64_t num_slots,
+    const int32_t* prefix_slots, const int32_t* prefix_offsets, const int32_t* group_offsets,
+    int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group,
+    const int32_t* slot_idx, const int32_t* seq_offsets, int32_t B,
+    int32_t total_tokens, int32_t max_len,
+    int32_t Hq, int32_t Hkv, int32_t D, float softmax_scale,
+    void* O, float* LSE,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+size_t esp_decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix,
+                                         int32_t max_group, int32_t total_tokens, int32_t max_len,
+                                         int32_t Hq, int32_t Hkv, int32_t D);
+
+/*
+ * What new queries and keys go through between their projection and attention,
+ * in one pass over them: the norm of every head (where there are weights)
+ *   y = x / sqrt(mean(x^2) + eps) * weight          (over the head's 128 elements)
+ * the rotation of its first `rot` elements by the token's position
+ *   (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t_i = q_pos * inv_freq[i],
+ * pair i being elements i and i + rot / 2, or with interleaved != 0 elements 2i and
+ * 2i + 1, and the append: K (rotated) and V go to their pool slots as in
+ * esp_kv_append.  All arithmetic is fp32, the angle fp64 (a position of 2^20 leaves an
+ * fp32 angle a tenth of a radian off); each result is rounded to bf16 once.
+ *
+ *   q [T,Hq,D], k, v [T,Hkv,D] bf16, a token's heads dense, consecutive tokens
+ *     q_stride, k_stride, v_stride elements apart (multiples of 8, at least a
+ *     token's heads): q, k and v may be parts of one projection's rows.
+ *   q_pos int32 [T]; inv_freq float [rot / 2].  rot = 0: no rotation, both may be NULL.  rot is
+ *     even and at most D, without interleaved a multiple of 16.
+ *   q_weight, k_weight bf16 [D] or NULL (that norm is left out); eps >= 0.
+ *   q_out bf16 [T,Hq,D], tokens q_out_stride elements apart; may be q itself (with q_stride).
+ *   k_out, v_out bf16 [T,Hkv,D] dense, or NULL: the rows for a prefill call.  May be k and v themselves where those are dense.
+ *   slot_idx int32 [T], k_pool, v_pool [num_slots,Hkv,D]: all NULL, or rows with a
+ *     slot in [0, num_slots) are written there (slots must be distinct).
+ * Outputs overlap their input only where they are it, and nothing else (a different overlap of q_out with
+ * q, k_out with k or v_out with v is refused, ESP_ERR_INVALID_ARG).  Bulk pointers and
+ * weights lie on 16 bytes (ESP_ERR_INVALID_ARG).
+ */
+esp_status esp_qk_norm_rope_append(
+    const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+    const int32_t* q_pos, const float* inv_freq, int32_t rot, int32_t interleaved,
+    const void* q_weight, const void* k_weight, float eps,
+    int32_t T, int32_t Hq, int32_t Hkv, int32_t D,
+    void* q_out, int64_t q_out_stride, void* k_out, void* v_out,
+    const int32_t* slot_idx, void* k_pool, void* v_pool, int64_t num_slots, void* stream);
+
+/*
+ * Block tables and slot lists from request lengths, on the GPU: what a serving step
+ * otherwise builds on the host and copies over.  A block table int32 [rows, width] names
+ * the pages of each request in order, page p holding the pool slots p * page ..
+ * p * page + page - 1 (page = 1: a pool of single tokens); -1: no page.  Request b of
+ * a call is row req_row[b] (NULL: row b).  A row outside the table has no tokens' pages.
+ *
+ * esp_extend_block_table gives the requests the pages that their tokens
+ * old_lens[b] .. new_lens[b] - 1 need, ceil(new / page) - ceil(old / page) each (none
+ * where that is negative; none past the table's width), in order of the requests
+ * from free_pages [n_free] on; an entry for which that holds no page any more gets -1.  Entries
+ * of tokens that the requests hold stay as they are.  pages_taken int32 [B+1]: request b got free_pages[
+ * pages_taken[b] .. pages_taken[b+1]); pages_taken[B] > n_free says that they
+ * did not suffice.  The rows of a call must be distinct.
+ *
+ * esp_build_slots lists the slots of tokens first_token[b] (NULL: 0) .. lens[b] - 1 of the
+ * requests, one request after another, in the form that decode, append, gather and
+ * prefill over the pool take.  keep_last > 0: of those only the last keep_last before lens[b], and of the first
+ * keep_first of the request (a sliding window behind a few first tokens).  A token
+ * without a page has slot -1 (append: not kept; gather: zeros; attention over such a list is undefined).
+ *   seq_offsets int32 [B+1]; slot_idx int32 [capacity]; token_pos int32 [capacity] or NULL: pos_first +
+ *   pos_stride * (the token's number in its request): global positions of striped shards.
+ *   A list longer than `capacity` is cut there, its offsets too (they never exceed
+ *   capacity); entries past seq_offsets[B] stay as they were.
+ * Lengths below 0 count as 0.  B = 0 writes the single offset 0.
+ */
+esp_status esp_extend_block_table(
+    const int32_t* free_pages, int32_t n_free, const int32_t* req_row,
+    const int32_t* old_lens, const int32_t* new_lens, int32_t B, int32_t page,
+    int32_t* block_table, int32_t rows, int32_t width, int32_t* pages_taken, void* stream);
+
+esp_status esp_build_slots(
+    const int32_t* block_table, int32_t rows, int32_t width, int32_t page, const int32_t* req_row,
+    const int32_t* first_token, const int32_t* lens, int32_t B,
+    int32_t keep_first, int32_t keep_last, int32_t pos_first, int32_t pos_stride,
+    int32_t capacity, int32_t* seq_offsets, int32_t* slot_idx, int32_t* token_pos, void* stream);
 
 /*
  * Measurement aids (no part of the method): what this GPU sustains on the two

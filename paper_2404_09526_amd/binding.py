@@ -32,6 +32,8 @@ EXPORTS = (
     "esp_debug_prefill_plan_for", "esp_debug_set_decode_plan", "esp_debug_decode_plan",
     "esp_partial_attn_decode_static", "esp_partial_attn_prefill_retain", "esp_plan_prefill_batches_monotone",
     "esp_partial_attn_decode_merge", "esp_partial_attn_prefill_pool_direct",
+    "esp_partial_attn_decode_shared", "esp_decode_shared_workspace_bytes", "esp_qk_norm_rope_append", "esp_extend_block_table",
+    "esp_build_slots",
 )
 ESP_DECODE_STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -80,6 +82,16 @@ def _load() -> ctypes.CDLL:
     L.esp_partial_attn_decode_merge.restype = i32
     L.esp_partial_attn_decode_static.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, vp]
     L.esp_partial_attn_decode_static.restype = i32
+    L.esp_partial_attn_decode_shared.argtypes = [vp, vp, vp, i64, vp, vp, vp] + [i32] * 4 + [vp, vp] + [i32] * 6 + [f32, vp, vp, vp, sz, vp]
+    L.esp_partial_attn_decode_shared.restype = i32
+    L.esp_decode_shared_workspace_bytes.argtypes = [i32] * 10
+    L.esp_decode_shared_workspace_bytes.restype = sz
+    L.esp_qk_norm_rope_append.argtypes = [vp] * 3 + [i64] * 3 + [vp, vp, i32, i32, vp, vp, f32] + [i32] * 4 + [vp, i64, vp, vp, vp, vp, vp, i64, vp]
+    L.esp_qk_norm_rope_append.restype = i32
+    L.esp_extend_block_table.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, i32, i32, vp, vp]
+    L.esp_extend_block_table.restype = i32
+    L.esp_build_slots.argtypes = [vp, i32, i32, i32, vp, vp, vp] + [i32] * 6 + [vp] * 4
+    L.esp_build_slots.restype = i32
     L.esp_decode_workspace_bytes.argtypes = [i32] * 6
     L.esp_decode_workspace_bytes.restype = sz
     L.esp_merge_partials.argtypes = [vp, vp, i32, i32, i32, i32, vp, vp, vp]
@@ -414,6 +426,190 @@ def esp_partial_attn_decode_merge(q, k_pool, v_pool, slot_idx, seq_offsets, max_
                                              total, int(max_len), Hq, Hkv, D, float(softmax_scale), op, lp, P,
                                              _ptr(O), _ptr(LSE), _ptr(_scratch(workspace)), workspace.numel(), _stream()))
     return O, LSE
+
+
+def _int32(x, name: str) -> int:
+    """A size that the C ABI takes in 32 bits (ctypes would cut it)."""
+    x = int(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return x
+
+
+def _one_device(*tensors) -> None:
+    """All of a call's tensors on the device that is current, whose stream it goes to."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def esp_decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, max_len, Hq, Hkv, D) -> int:
+    return int(lib.esp_decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, max_len, Hq, Hkv, D))
+
+
+def esp_partial_attn_decode_shared(q, k_pool, v_pool, prefix_slots, prefix_offsets, group_offsets, max_prefix, max_group, slot_idx, seq_offsets,
+                                   max_len, softmax_scale=None, O=None, LSE=None, workspace=None):
+    """Decode of requests in groups (group g: requests group_offsets[g] .. group_offsets[g+1] - 1) that share a prefix: request b attends the
+    pool rows prefix_slots[prefix_offsets[g] .. prefix_offsets[g+1]) of its group and its own, slot_idx[seq_offsets[b] .. seq_offsets[b+1]).
+    A group's prefix is read once.  q [B,Hq,D] bf16, pools [S,Hkv,D] bf16, lists and offsets int32; max_prefix, max_group, max_len: bounds of a
+    prefix's tokens, a group's requests and a request's own tokens.  Returns (O bf16 [B,Hq,D], LSE fp32 [B,Hq])."""
+    _dev(q, torch.bfloat16, "q"); _dev(k_pool, torch.bfloat16, "k_pool"); _dev(v_pool, torch.bfloat16, "v_pool")
+    for t, name in ((prefix_slots, "prefix_slots"), (prefix_offsets, "prefix_offsets"), (group_offsets, "group_offsets"), (slot_idx, "slot_idx"),
+                    (seq_offsets, "seq_offsets")):
+        _dev(t, torch.int32, name)
+    if q.dim() != 3 or k_pool.dim() != 3:
+        raise ValueError("decode (shared): shape mismatch")
+    B, Hq, D = q.shape
+    S, Hkv, Dk = k_pool.shape
+    n_groups = group_offsets.numel() - 1
+    if v_pool.shape != k_pool.shape or Dk != D or seq_offsets.numel() != B + 1 or n_groups < 0 or prefix_offsets.numel() != n_groups + 1:
+        raise ValueError("decode (shared): shape mismatch")
+    prefix_total, total = prefix_slots.numel(), slot_idx.numel()
+    for x, name in ((prefix_total, "prefix_slots"), (total, "slot_idx"), (max_prefix, "max_prefix"), (max_group, "max_group"), (max_len, "max_len")):
+        _int32(x, name)
+    max_prefix, max_group, max_len = int(max_prefix), int(max_group), int(max_len)
+    if softmax_scale is None:
+        softmax_scale = D ** -0.5
+    if O is None:
+        O = torch.empty_like(q)
+    if LSE is None:
+        LSE = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+    _out(O, torch.bfloat16, B * Hq * D, "O"); _out(LSE, torch.float32, B * Hq, "LSE")
+    if workspace is None:
+        workspace = _workspace(esp_decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total, max_len, Hq, Hkv, D), q.device)
+    _scratch(workspace)
+    _one_device(q, k_pool, v_pool, prefix_slots, prefix_offsets, group_offsets, slot_idx, seq_offsets, O, LSE, workspace)
+    _check(lib.esp_partial_attn_decode_shared(_ptr(q), _ptr(k_pool), _ptr(v_pool), S, _ptr(prefix_slots), _ptr(prefix_offsets), _ptr(group_offsets),
+                                              n_groups, prefix_total, max_prefix, max_group, _ptr(slot_idx), _ptr(seq_offsets), B, total, max_len,
+                                              Hq, Hkv, D, float(softmax_scale), _ptr(O), _ptr(LSE), _ptr(workspace),
+                                              workspace.numel() * workspace.element_size(), _stream()))
+    return O, LSE
+
+
+def _heads(t: torch.Tensor, name: str):
+    """[T, H, D] bf16 on the device with a token's heads dense.  Returns (T, H, D, elements from a token to the next)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must live in device memory")
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name}: must be [tokens, heads, elements]")
+    T, H, D = t.shape
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: a token's heads must be dense")
+    return T, H, D, t.stride(0) if T > 1 else H * D
+
+
+def esp_qk_norm_rope_append(q, k, v, q_pos=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, slot_idx=None,
+                            k_pool=None, v_pool=None, q_out=None, k_out=None, v_out=None):
+    """Norm (weights bf16 [D], where given) and rotation (by q_pos int32 [T] times inv_freq fp32 [rot/2], where given) of new queries q [T,Hq,D]
+    and keys k [T,Hkv,D], and the append of k and v to the pool rows slot_idx (where given; a slot outside the pool: not kept).  q, k, v and q_out may be
+    parts of one projection's rows; q_out may be q.  k_out, v_out: dense rows, written where given.  Returns (q_out, k_out, v_out)."""
+    T, Hq, D, q_stride = _heads(q, "q")
+    Tk, Hkv, Dk, k_stride = _heads(k, "k")
+    Tv, Hv, Dv, v_stride = _heads(v, "v")
+    if not (T == Tk == Tv and D == Dk == Dv and Hkv == Hv):
+        raise ValueError("norm and rotation: shape mismatch")
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=torch.bfloat16, device=q.device)
+    To, Ho, Do, q_out_stride = _heads(q_out, "q_out")
+    if (To, Ho, Do) != (T, Hq, D):
+        raise ValueError("norm and rotation: q_out has another shape than q")
+    rot = 0
+    if inv_freq is not None:
+        _dev(inv_freq, torch.float32, "inv_freq")
+        if q_pos is None:
+            raise ValueError("norm and rotation: a rotation needs q_pos")
+        rot = 2 * inv_freq.numel()
+    if q_pos is not None:
+        _dev(q_pos, torch.int32, "q_pos")
+        if q_pos.shape != (T,):
+            raise ValueError("norm and rotation: q_pos must be [tokens]")
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _dev(w, torch.bfloat16, name)
+            if w.shape != (D,):
+                raise ValueError(f"norm and rotation: {name} must be [{D}]")
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is not None:
+            _dev(t, torch.bfloat16, name)
+            if t.shape != k.shape:
+                raise ValueError(f"norm and rotation: {name} has another shape than k")
+    S = 0
+    if slot_idx is not None:
+        if k_pool is None or v_pool is None:
+            raise ValueError("norm and rotation: slot_idx needs both pools")
+        _dev(slot_idx, torch.int32, "slot_idx"); _dev(k_pool, torch.bfloat16, "k_pool"); _dev(v_pool, torch.bfloat16, "v_pool")
+        if slot_idx.shape != (T,) or k_pool.dim() != 3 or k_pool.shape[1:] != k.shape[1:] or v_pool.shape != k_pool.shape:
+            raise ValueError("norm and rotation: slots or pools of another shape than the rows")
+        S = k_pool.shape[0]
+    elif k_pool is not None or v_pool is not None:
+        raise ValueError("norm and rotation: the pools need slot_idx")
+    _one_device(q, k, v, q_pos, inv_freq, q_weight, k_weight, slot_idx, k_pool, v_pool, q_out, k_out, v_out)
+    _check(lib.esp_qk_norm_rope_append(_ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride, _ptr(q_pos), _ptr(inv_freq), rot,
+                                       int(bool(interleaved)), _ptr(q_weight), _ptr(k_weight), float(eps), T, Hq, Hkv, D, _ptr(q_out), q_out_stride,
+                                       _ptr(k_out), _ptr(v_out), _ptr(slot_idx), _ptr(k_pool), _ptr(v_pool), S, _stream()))
+    return q_out, k_out, v_out
+
+
+def _table(block_table, lens, req_row, what: str):
+    """Checks what the calls on block tables share; returns (requests, rows, width)."""
+    _dev(block_table, torch.int32, "block_table"); _dev(lens, torch.int32, what)
+    if block_table.dim() != 2 or lens.dim() != 1:
+        raise ValueError(f"block_table must be [rows, pages], {what} [requests]")
+    B, (rows, width) = lens.numel(), block_table.shape
+    if req_row is not None:
+        _dev(req_row, torch.int32, "req_row")
+        if req_row.shape != (B,):
+            raise ValueError("req_row must be [requests]")
+    elif B > rows:
+        raise ValueError("block_table has fewer rows than there are requests")
+    return B, rows, width
+
+
+def esp_extend_block_table(block_table, free_pages, old_lens, new_lens, page, req_row=None, pages_taken=None):
+    """Gives the requests the pages that their tokens old_lens[b] .. new_lens[b] - 1 need, from free_pages on, in block_table int32 [rows, pages]
+    (in place; request b is row req_row[b], or row b).  Entries that free_pages is too short for become -1.  Returns pages_taken int32
+    [B+1]: request b got free_pages[pages_taken[b] .. pages_taken[b+1])."""
+    B, rows, width = _table(block_table, old_lens, req_row, "old_lens")
+    _dev(new_lens, torch.int32, "new_lens"); _dev(free_pages, torch.int32, "free_pages")
+    if new_lens.shape != (B,) or free_pages.dim() != 1:
+        raise ValueError("block table: old_lens and new_lens must be [requests], free_pages one list")
+    if pages_taken is None:
+        pages_taken = torch.empty(B + 1, dtype=torch.int32, device=block_table.device)
+    _out(pages_taken, torch.int32, B + 1, "pages_taken")
+    _one_device(block_table, free_pages, old_lens, new_lens, req_row, pages_taken)
+    _check(lib.esp_extend_block_table(_ptr(free_pages), _int32(free_pages.numel(), "free_pages"), _ptr(req_row), _ptr(old_lens), _ptr(new_lens), B, _int32(page, "page"),
+                                      _ptr(block_table), rows, width, _ptr(pages_taken), _stream()))
+    return pages_taken
+
+
+def esp_build_slots(block_table, lens, page, first_token=None, req_row=None, keep_first=0, keep_last=0, pos_first=0, pos_stride=1, capacity=None,
+                    seq_offsets=None, slot_idx=None, token_pos=None):
+    """The slots of tokens first_token[b] (or 0) .. lens[b] - 1 of the requests, one request after another; with keep_last > 0 of those only
+    the last keep_last and the first keep_first of the request.  The list is written to slot_idx (all of it is room), or to a new one of `capacity`
+    entries; token_pos, where given, receives pos_first + pos_stride * token.  Returns (seq_offsets int32 [B+1], slot_idx, token_pos)."""
+    B, rows, width = _table(block_table, lens, req_row, "lens")
+    if first_token is not None:
+        _dev(first_token, torch.int32, "first_token")
+        if first_token.shape != (B,):
+            raise ValueError("slot list: first_token must be [requests]")
+    if seq_offsets is None:
+        seq_offsets = torch.empty(B + 1, dtype=torch.int32, device=block_table.device)
+    if slot_idx is None:
+        if capacity is None:
+            raise ValueError("slot list: slot_idx or a capacity is needed")
+        slot_idx = torch.empty(int(capacity), dtype=torch.int32, device=block_table.device)
+    capacity = slot_idx.numel() if capacity is None else int(capacity)
+    _out(seq_offsets, torch.int32, B + 1, "seq_offsets"); _out(slot_idx, torch.int32, capacity, "slot_idx")
+    if token_pos is not None:
+        _out(token_pos, torch.int32, capacity, "token_pos")
+    _one_device(block_table, lens, first_token, req_row, seq_offsets, slot_idx, token_pos)
+    _check(lib.esp_build_slots(_ptr(block_table), rows, width, _int32(page, "page"), _ptr(req_row), _ptr(first_token), _ptr(lens), B,
+                               _int32(keep_first, "keep_first"), _int32(keep_last, "keep_last"), _int32(pos_first, "pos_first"),
+                               _int32(pos_stride, "pos_stride"), _int32(capacity, "capacity"), _ptr(seq_offsets), _ptr(slot_idx), _ptr(token_pos), _stream()))
+    return seq_offsets, slot_idx, token_pos
 
 
 def esp_merge_partials(O_parts: Sequence[torch.Tensor], LSE_parts: Sequence[torch.Tensor], O=None, LSE=None,

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "esp_common.h"
+#include "rotate.h"
 
 namespace esp {
 
@@ -358,6 +359,141 @@ esp_status esp_partial_attn_decode_merge(const void* q, const void* k_pool, cons
     if (st != ESP_OK) return st;
     return launch_decode(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, max_len, Hq, Hkv, softmax_scale, O, LSE,
                          workspace, workspace_bytes, (hipStream_t)stream, &peers, n_peers);
+}
+
+size_t esp_decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group,
+                                         int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, int32_t D) {
+    (void)max_len;
+    if (B < 0 || n_groups < 0 || prefix_total < 0 || max_prefix < 0 || max_prefix > prefix_total || max_group < 0 || max_group > B ||
+        (n_groups == 0 && prefix_total > 0) || total_tokens < 0 || !decode_heads_supported(Hq, Hkv) || D != kHeadDim)
+        return 0;
+    return decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv);
+}
+
+esp_status esp_partial_attn_decode_shared(const void* q, const void* k_pool, const void* v_pool, int64_t num_slots,
+                                          const int32_t* prefix_slots, const int32_t* prefix_offsets, const int32_t* group_offsets,
+                                          int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group,
+                                          const int32_t* slot_idx, const int32_t* seq_offsets, int32_t B, int32_t total_tokens,
+                                          int32_t max_len, int32_t Hq, int32_t Hkv, int32_t D, float softmax_scale, void* O, float* LSE,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+    bool done;
+    esp_status st = decode_check(q, k_pool, v_pool, num_slots, slot_idx, seq_offsets, B, total_tokens, max_len, Hq, Hkv, D,
+                                 softmax_scale, O, LSE, &done);
+    if (st != ESP_OK) return st;
+    if (n_groups < 0 || prefix_total < 0 || max_prefix < 0 || max_group < 0) return fail(ESP_ERR_INVALID_ARG, "decode (shared): negative size");
+    if (max_prefix > prefix_total) return fail(ESP_ERR_INVALID_ARG, "decode (shared): max_prefix exceeds prefix_total");
+    if (max_group > B) return fail(ESP_ERR_INVALID_ARG, "decode (shared): max_group exceeds B");
+    if (n_groups == 0 && prefix_total > 0) return fail(ESP_ERR_INVALID_ARG, "decode (shared): a prefix without a group");
+    if (done) return ESP_OK;
+    if (n_groups > 0 && (!prefix_offsets || !group_offsets)) return fail(ESP_ERR_INVALID_ARG, "decode (shared): null prefix_offsets/group_offsets");
+    if (prefix_total > 0 && (!k_pool || !v_pool || !prefix_slots || num_slots == 0))
+        return fail(ESP_ERR_INVALID_ARG, "decode (shared): null pool/prefix_slots");
+    const size_t need = decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv);
+    if (!workspace || workspace_bytes < need)
+        return fail(ESP_ERR_WORKSPACE, "decode (shared): workspace needs %zu bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
+    if ((uintptr_t)workspace & 255) return fail(ESP_ERR_WORKSPACE, "decode (shared): workspace not 256-byte aligned");
+    if (debug_validate()) {
+        st = decode_validate(slot_idx, seq_offsets, B, total_tokens, max_len, num_slots, stream);
+        if (st == ESP_OK && n_groups > 0) st = check_offsets("decode (shared): group_offsets", group_offsets, n_groups, B, max_group, (hipStream_t)stream);
+        if (st == ESP_OK && n_groups > 0) st = check_offsets("decode (shared): prefix_offsets", prefix_offsets, n_groups, prefix_total, max_prefix, (hipStream_t)stream);
+        if (st == ESP_OK) st = check_slots("decode (shared): prefix", prefix_slots, prefix_total, num_slots, false, false, (hipStream_t)stream);
+        if (st != ESP_OK) return st;
+    }
+    const SharedArgs a = {q, (const char*)k_pool, (const char*)v_pool, prefix_slots, prefix_offsets, group_offsets, n_groups, prefix_total,
+                          max_prefix, max_group, slot_idx, seq_offsets, B, total_tokens, max_len, Hq, Hkv, softmax_scale, O, LSE};
+    return launch_decode_shared(a, workspace, (hipStream_t)stream);
+}
+
+// an output that shares memory with its input without being it
+static bool halfway(const void* out, int64_t out_stride, const void* in, int64_t in_stride, int64_t T, int64_t row) {
+    if (out == in && out_stride == in_stride) return false;
+    const char *a = (const char*)out, *b = (const char*)in;
+    return a < b + ((T - 1) * in_stride + row) * 2 && b < a + ((T - 1) * out_stride + row) * 2;
+}
+
+esp_status esp_qk_norm_rope_append(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                   const int32_t* q_pos, const float* inv_freq, int32_t rot, int32_t interleaved, const void* q_weight,
+                                   const void* k_weight, float eps, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, void* q_out,
+                                   int64_t q_out_stride, void* k_out, void* v_out, const int32_t* slot_idx, void* k_pool, void* v_pool,
+                                   int64_t num_slots, void* stream) {
+    if (T < 0 || num_slots < 0) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: negative size");
+    if (!heads_ok(Hq, Hkv)) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: Hq=%d must be a positive multiple of Hkv=%d", Hq, Hkv);
+    if (D != kHeadDim) return fail(ESP_ERR_UNSUPPORTED, "norm and rotation: head_dim %d unsupported (only 128)", D);
+    if (rot < 0 || rot > D || rot % 2 != 0) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: rot=%d must be even and within 0..%d", rot, D);
+    if (!interleaved && rot % 16 != 0) return fail(ESP_ERR_UNSUPPORTED, "norm and rotation: rot=%d must be a multiple of 16 where halves are paired", rot);
+    if (!(eps >= 0.f) || eps > 3e38f) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: bad eps");
+    const int64_t q_row = (int64_t)Hq * D, k_row = (int64_t)Hkv * D, strides[4] = {q_stride, k_stride, v_stride, q_out_stride};
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = i == 0 || i == 3 ? q_row : k_row;
+        if (strides[i] < row || strides[i] % 8 != 0)
+            return fail(ESP_ERR_INVALID_ARG, "norm and rotation: a stride of %lld must be a multiple of 8 and at least a token's %lld elements", (long long)strides[i], (long long)row);
+        if (strides[i] > INT64_MAX / 4 / (T > 0 ? T : 1)) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: a stride of %lld is too large", (long long)strides[i]);
+    }
+    if (T == 0) return ESP_OK;
+    if (!q || !k || !v || !q_out) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: null q/k/v/q_out");
+    if (rot > 0 && (!q_pos || !inv_freq)) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: null q_pos/inv_freq");
+    if ((slot_idx == nullptr) != (k_pool == nullptr) || (slot_idx == nullptr) != (v_pool == nullptr))
+        return fail(ESP_ERR_INVALID_ARG, "norm and rotation: slot_idx and the pools must all be given or all be NULL");
+    if (slot_idx && num_slots == 0) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: empty pool");
+    for (const void* p : {q, k, v, q_weight, k_weight, (const void*)q_out, (const void*)k_out, (const void*)v_out, (const void*)k_pool, (const void*)v_pool})
+        if ((uintptr_t)p & 15) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: a pointer is not 16-byte aligned");
+    if (halfway(q_out, q_out_stride, q, q_stride, T, q_row) || (k_out && halfway(k_out, k_row, k, k_stride, T, k_row)) ||
+        (v_out && halfway(v_out, k_row, v, v_stride, T, k_row)))
+        return fail(ESP_ERR_INVALID_ARG, "norm and rotation: an output overlaps its input without being it");
+    if (slot_idx && debug_validate()) {
+        const esp_status st = check_slots("norm and rotation", slot_idx, T, num_slots, true, true, (hipStream_t)stream);
+        if (st != ESP_OK) return st;
+    }
+    RotateArgs a = {(const char*)q, (const char*)k, (const char*)v, q_stride, k_stride, v_stride, q_out_stride, q_pos, inv_freq, (const char*)q_weight,
+                    (const char*)k_weight, (char*)q_out, (char*)k_out, (char*)v_out, slot_idx, (char*)k_pool, (char*)v_pool, num_slots, T, Hq, Hkv, rot, eps, 1, 0};
+    return launch_rotate(a, interleaved, (hipStream_t)stream);
+}
+
+// what both calls on block tables are asked
+static esp_status table_check(const char* what, const int32_t* table, int32_t rows, int32_t width, int32_t page, int32_t B) {
+    if (B < 0 || rows < 0 || width < 0) return fail(ESP_ERR_INVALID_ARG, "%s: negative size", what);
+    if (page < 1) return fail(ESP_ERR_INVALID_ARG, "%s: page=%d must be at least 1", what, page);
+    if (rows > 0 && width > 0 && !table) return fail(ESP_ERR_INVALID_ARG, "%s: null block_table", what);
+    return ESP_OK;
+}
+// rows of a call: distinct (where they are written), or at least inside the table
+static esp_status check_rows(const char* what, const int32_t* dev, int32_t B, int32_t rows, bool unique, hipStream_t stream) {
+    std::vector<int32_t> h;
+    if (!fetch_i32(dev, (size_t)B, stream, h)) return fail(ESP_ERR_HIP, "%s: cannot read req_row back", what);
+    for (int32_t i = 0; i < B; ++i)
+        if (h[i] < 0 || h[i] >= rows) return fail(ESP_ERR_INVALID_ARG, "%s: req_row[%d] = %d is outside the table's %d rows", what, i, h[i], rows);
+    std::sort(h.begin(), h.end());
+    for (int32_t i = 1; unique && i < B; ++i)
+        if (h[i] == h[i - 1]) return fail(ESP_ERR_INVALID_ARG, "%s: row %d is named twice", what, h[i]);
+    return ESP_OK;
+}
+
+esp_status esp_extend_block_table(const int32_t* free_pages, int32_t n_free, const int32_t* req_row, const int32_t* old_lens,
+                                  const int32_t* new_lens, int32_t B, int32_t page, int32_t* block_table, int32_t rows, int32_t width,
+                                  int32_t* pages_taken, void* stream) {
+    esp_status st = table_check("block table", block_table, rows, width, page, B);
+    if (st != ESP_OK) return st;
+    if (n_free < 0) return fail(ESP_ERR_INVALID_ARG, "block table: negative size");
+    if (!pages_taken || (B > 0 && (!old_lens || !new_lens)) || (n_free > 0 && !free_pages))
+        return fail(ESP_ERR_INVALID_ARG, "block table: null pointer");
+    if (req_row && B > 0 && debug_validate()) st = check_rows("block table", req_row, B, rows, true, (hipStream_t)stream);
+    if (st != ESP_OK) return st;
+    return launch_extend_table(free_pages, n_free, req_row, old_lens, new_lens, B, page, block_table, rows, width, pages_taken, (hipStream_t)stream);
+}
+
+esp_status esp_build_slots(const int32_t* block_table, int32_t rows, int32_t width, int32_t page, const int32_t* req_row,
+                           const int32_t* first_token, const int32_t* lens, int32_t B, int32_t keep_first, int32_t keep_last,
+                           int32_t pos_first, int32_t pos_stride, int32_t capacity, int32_t* seq_offsets, int32_t* slot_idx,
+                           int32_t* token_pos, void* stream) {
+    esp_status st = table_check("slot list", block_table, rows, width, page, B);
+    if (st != ESP_OK) return st;
+    if (keep_first < 0 || keep_last < 0 || capacity < 0) return fail(ESP_ERR_INVALID_ARG, "slot list: negative size");
+    if (keep_first > 0 && keep_last == 0) return fail(ESP_ERR_INVALID_ARG, "slot list: keep_first needs a window, keep_last > 0");
+    if (!seq_offsets || (B > 0 && !lens) || (capacity > 0 && !slot_idx)) return fail(ESP_ERR_INVALID_ARG, "slot list: null pointer");
+    if (req_row && B > 0 && debug_validate()) st = check_rows("slot list", req_row, B, rows, false, (hipStream_t)stream);
+    if (st != ESP_OK) return st;
+    return launch_build_slots(block_table, rows, width, page, req_row, first_token, lens, B, keep_first, keep_last, pos_first, pos_stride, capacity,
+                              seq_offsets, slot_idx, token_pos, (hipStream_t)stream);
 }
 
 static esp_status merge_entry(const void* const* O_parts, const float* const* LSE_parts, int32_t P, int32_t T,
