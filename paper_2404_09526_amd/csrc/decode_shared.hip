@@ -25,10 +25,10 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_prefix_kernel(Sha
     const RequestRange at = request_range(blockIdx.x, parts.range, a.n_groups, a.prefix_offsets, lane);
     const int32_t t0 = at.t0, t1 = min(at.t1, a.prefix_total);      // (never past the slot list)
     const int32_t b0 = a.group_offsets[at.b], n_req = min(min(a.group_offsets[at.b + 1], a.B) - b0, a.max_group);
-    const int32_t rho0 = blockIdx.z * 32, n_rows = min(32, n_req * G - rho0);
+    const int32_t n_rows = n_req * G;                                // at most 32 in every group
     if (t0 >= t1 || n_rows <= 0) return;
     const int32_t seg = t1 - t0;
-    const int32_t rho = rho0 + min(qi, n_rows - 1), of = rho / G;
+    const int32_t rho = min(qi, n_rows - 1), of = rho / G;
     const int32_t row = of * a.Hq + kvh * G + (rho - of * G);         // within the group's queries
 
     const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
@@ -83,6 +83,116 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_prefix_kernel(Sha
 #pragma unroll
     for (int e = 0; e < 64 / kSharedWaves; e += 4) *(float4*)(dst + 2 * e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
     if (wave == 0 && hi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
+}
+
+// More columns than one tile has: a workgroup of eight wavefronts has COLS tiles of 32 of them, a wavefront one, and the COLS wavefronts that
+// have different columns (a team) share tiles of 32 keys in LDS, so that a row of K and V comes from memory once for 32 COLS columns; the 8 / COLS
+// teams take the tiles in turn.  All teams' tiles are a step; COLS steps are on their way or at work (128 KiB of LDS in every form), and one
+// barrier a step says both that its tiles are there and that the stage of the step before may be filled again.
+constexpr int kWideWaves = 8;
+constexpr int kWideTile = kColKBytes + kColVBytes;
+constexpr int kWideMost = 4096;                                     // keys of a range: its slots lie in LDS
+
+template <int COLS>
+__global__ __launch_bounds__(kWideWaves * 64, 2) void shared_wide_kernel(SharedArgs a, float scale_log2, SharedParts parts, int32_t units, int32_t col_blocks) {
+    constexpr int TEAMS = kWideWaves / COLS, STAGES = COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: transfers of K, and of V, of a wavefront a step
+    constexpr int kRing = STAGES * TEAMS * kWideTile, kLds = kRing + kWideMost * 4;
+    static_assert(kRing + 1 >= 128 * 1024 && kWideWaves * kColWaveBytes <= kLds, "the blocks of the combination fit");
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kLds];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int team = wave / COLS, ct = wave % COLS;
+    const int qi = lane & 31, hi = lane >> 5;
+    // unit: (range, KV head), heads next to each other as in a pool row.  The column blocks of a unit are eight workgroups apart: on one XCD, whose
+    // L2 then has the rows.
+    const uint32_t all = blockIdx.x, eight = all / (8u * col_blocks), rest = all - eight * (8u * col_blocks);
+    const uint32_t unit = eight * 8 + (rest & 7), cb = rest >> 3;
+    if (unit >= (uint32_t)units) return;
+    const int kvh = unit % (uint32_t)a.Hkv, G = a.Hq / a.Hkv;
+    const RequestRange at = request_range(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
+    const int32_t t0 = at.t0, t1 = min(at.t1, a.prefix_total);      // (never past the slot list)
+    const int32_t b0 = a.group_offsets[at.b], n_req = min(min(a.group_offsets[at.b + 1], a.B) - b0, a.max_group);
+    const int32_t seg = t1 - t0;
+    if (seg <= 0 || n_req * G <= (int32_t)cb * (32 * COLS)) return;
+    const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = min(32, n_req * G - rho0);   // (columns of this wavefront; none: it only moves tiles)
+
+    int32_t* const list = (int32_t*)(smem + kRing);
+    for (int i = threadIdx.x; i < seg; i += kWideWaves * 64) list[i] = a.prefix_slots[t0 + i];
+
+    const int32_t rho = rho0 + max(min(qi, n_rows - 1), 0), rho_in = min(rho, n_req * G - 1), of = rho_in / G;
+    const int32_t row = of * a.Hq + kvh * G + (rho_in - of * G);      // within the group's queries
+    bf16x8 qf[8];
+    const uint16_t* qp = (const uint16_t*)a.q + ((int64_t)b0 * a.Hq + row) * kHeadDim + 8 * hi;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        uint4 raw = *(const uint4*)(qp + 16 * t);
+        if (qi >= n_rows) raw = make_uint4(0u, 0u, 0u, 0u);
+        qf[t] = __builtin_bit_cast(bf16x8, raw);
+    }
+    asm volatile("" :: "v"(qf[0]), "v"(qf[1]), "v"(qf[2]), "v"(qf[3]), "v"(qf[4]), "v"(qf[5]), "v"(qf[6]), "v"(qf[7]));   // here before the transfers, whose waits count
+    __syncthreads();
+
+    const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
+    const char* kbase = a.k_pool + (uint32_t)kvh * (kHeadDim * 2);
+    const char* vbase = a.v_pool + (uint32_t)kvh * (kHeadDim * 2);
+    const uint32_t lds = (uint32_t)(uintptr_t)(ESP_LDS unsigned char*)smem;
+    const int steps = (seg + STEP - 1) / STEP;
+    auto fetch = [&](int i) {
+        const uint32_t to = lds + ((i % STAGES) * TEAMS + team) * kWideTile;
+        uint64_t row_at[MOVES];
+#pragma unroll
+        for (int x = 0; x < MOVES; ++x) {
+            const int n = ct + COLS * x;
+            row_at[x] = (uint64_t)(uint32_t)list[min(i * STEP + team * 32 + col_row(n, lane), seg - 1)] * row_bytes;
+            load_to_lds_b128_at(to + 1024 * n, kbase + (row_at[x] + col_k_within(n, lane)));
+        }
+#pragma unroll
+        for (int x = 0; x < MOVES; ++x) {
+            const int n = ct + COLS * x;
+            load_to_lds_b128_at(to + kColKBytes + 1024 * n, vbase + (row_at[x] + col_v_within(lane)));
+        }
+    };
+    // the transfers of step i have landed: those of up to STAGES - 2 steps after it may be on their way
+    auto landed = [&](int i) {
+        const int after = min(steps - 1 - i, STAGES - 2);
+        if (after <= 0) wait_vm<0>();
+        else if (after == 1) wait_vm<2 * MOVES>();
+        else if (after == 2) wait_vm<4 * MOVES>();
+        else if (after == 3) wait_vm<6 * MOVES>();
+        else if (after == 4) wait_vm<8 * MOVES>();
+        else if (after == 5) wait_vm<10 * MOVES>();
+        else wait_vm<12 * MOVES>();
+    };
+    for (int i = 0; i < STAGES - 1 && i < steps; ++i) fetch(i);
+
+    Columns cols;
+    cols.clear();
+    for (int i = 0; i < steps; ++i) {
+        landed(i);
+        wg_barrier();
+        if (i + STAGES - 1 < steps) fetch(i + STAGES - 1);
+        const int here = seg - i * STEP - team * 32;                // keys of this tile
+        if (n_rows <= 0 || here <= 0) continue;
+        cols.place(lds + ((i % STAGES) * TEAMS + team) * kWideTile, lane);
+        floatx16 sc = cols.scores(qf);
+        if (here < 32) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
+        }
+        Columns::PFrag pf[2];
+        cols.weigh(sc, scale_log2, pf);
+        cols.accumulate(pf);
+    }
+    float out[64 / TEAMS], mx, lsum;
+    __syncthreads();                                                // the ring is read: it may hold the teams' results
+    cols.combine<TEAMS, COLS>(smem + ct * kColWaveBytes, team, lane, out, mx, lsum);
+    if (qi >= n_rows) return;
+    const int64_t ph = (int64_t)(at.w + at.b) * a.max_group * a.Hq + row;
+    float* dst = parts.acc + ph * kHeadDim + Columns::first_element<TEAMS>(team, lane);
+#pragma unroll
+    for (int e = 0; e < 64 / TEAMS; e += 4) *(float4*)(dst + 2 * e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
+    if (team == 0 && hi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
 }
 
 // Combination, as the plain decode's (decode.hip): groups of 32 lanes take a pair's partials in turn, four at a time, first those of the
@@ -159,15 +269,33 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
     if (lane == 0) a.LSE[pair] = Lt == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(Lt)) * kLn2;
 }
 
-// ranges of the prefix lists, and the partials' slots
-static int32_t shared_range(int32_t prefix_total, int32_t max_group, int32_t Hq, int32_t Hkv) {
-    const int64_t blocks = ((int64_t)max_group * (Hq / Hkv) + 31) / 32;
-    return decode_range(prefix_total, kSharedWaves * 32, 1, Hkv * blocks, 1, 1 << 20);
+// Ranges of the prefix lists, which kernel has them, and the partials' slots.
+struct SharedPlan { int32_t cols, range; };                         // cols: column tiles of a workgroup; 1: the kernel for one
+static SharedPlan shared_plan(int32_t prefix_total, int32_t max_group, int32_t Hq, int32_t Hkv) {
+    const int64_t rows = (int64_t)max_group * (Hq / Hkv);
+    if (rows <= 32) return {1, decode_range(prefix_total, kSharedWaves * 32, 1, Hkv, 1, 1 << 20)};
+    const int32_t cols = rows <= 64 ? 2 : rows <= 128 ? 4 : 8, step = 32 * (kWideWaves / cols);
+    // One workgroup a CU.  Of the ranges that fill 1 .. 16 rounds of them the one whose rounds, each with a start, an end (its partial, written and
+    // read) and its steps, take the least time.
+    constexpr int64_t kResident = 256;
+    const double start = 6 + 0.04 * 32 * cols, per_step = 0.63 * (kWideWaves / cols);
+    const int64_t steps = ((int64_t)prefix_total + step - 1) / step, units = Hkv * ((rows + 32 * cols - 1) / (32 * cols));
+    int64_t best = 1;
+    double best_us = 0;
+    for (int64_t rounds = 1; rounds <= 16; ++rounds) {
+        const int64_t fit = rounds * kResident / units;
+        int64_t take = fit > 0 ? (steps + fit - 1) / fit : steps;
+        if (take > kWideMost / step) take = kWideMost / step;
+        const int64_t wgs = (steps + take - 1) / take * units;
+        const double us = (double)((wgs + kResident - 1) / kResident) * (start + per_step * (double)take);
+        if (rounds == 1 || us < best_us) { best = take; best_us = us; }
+    }
+    return {cols, (int32_t)(best * step)};
 }
 static size_t shared_slots(int32_t n_groups, int32_t prefix_total, int32_t range) { return prefix_total > 0 ? (size_t)(prefix_total / range) + n_groups : 0; }
 static size_t shared_prefix_bytes(int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t Hq, int32_t Hkv) {
     if (prefix_total <= 0) return 0;
-    const size_t slots = shared_slots(n_groups, prefix_total, shared_range(prefix_total, max_group, Hq, Hkv));
+    const size_t slots = shared_slots(n_groups, prefix_total, shared_plan(prefix_total, max_group, Hq, Hkv).range);
     return (slots * max_group * Hq * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256;
 }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
@@ -183,15 +311,25 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     char* mine_at = (char*)workspace;
     int64_t most = 0;                                               // partials of a pair
     if (a.prefix_total > 0 && a.max_group > 0) {
-        parts.range = shared_range(a.prefix_total, a.max_group, a.Hq, a.Hkv);
+        const SharedPlan plan = shared_plan(a.prefix_total, a.max_group, a.Hq, a.Hkv);
+        parts.range = plan.range;
         const size_t slots = shared_slots(a.n_groups, a.prefix_total, parts.range);
         parts.ml = parts.acc + slots * a.max_group * a.Hq * kHeadDim;
         mine_at += shared_prefix_bytes(a.n_groups, a.prefix_total, a.max_group, a.Hq, a.Hkv);
         most = a.max_prefix / parts.range + 1;
-        const int64_t blocks = ((int64_t)a.max_group * G + 31) / 32;
-        if (a.Hkv > 65535 || blocks > 65535 || slots > UINT32_MAX / (kSharedWaves * 64)) return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
-        hipLaunchKernelGGL(shared_prefix_kernel, dim3((unsigned)slots, a.Hkv, (unsigned)blocks), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, parts);
-        const esp_status st = check_launch("shared_prefix_kernel");
+        const int64_t tiles = ((int64_t)a.max_group * G + 31) / 32, blocks = (tiles + plan.cols - 1) / plan.cols, units = (int64_t)slots * a.Hkv;
+        if (a.Hkv > 65535 || blocks * ((units + 7) / 8 * 8) > UINT32_MAX / (kWideWaves * 64))
+            return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
+        const float sl2 = a.softmax_scale * kLog2e;
+#define ESP_WIDE_LAUNCH(COLS)                                                                                                               \
+    hipLaunchKernelGGL(shared_wide_kernel<COLS>, dim3((unsigned)((units + 7) / 8 * 8 * blocks)), dim3(kWideWaves * 64), 0, stream, a, sl2, parts, \
+                       (int32_t)units, (int32_t)blocks)
+        if (plan.cols == 1) hipLaunchKernelGGL(shared_prefix_kernel, dim3((unsigned)slots, a.Hkv), dim3(kSharedWaves * 64), 0, stream, a, sl2, parts);
+        else if (plan.cols == 2) ESP_WIDE_LAUNCH(2);
+        else if (plan.cols == 4) ESP_WIDE_LAUNCH(4);
+        else ESP_WIDE_LAUNCH(8);
+#undef ESP_WIDE_LAUNCH
+        const esp_status st = check_launch(plan.cols == 1 ? "shared_prefix_kernel" : "shared_wide_kernel");
         if (st != ESP_OK) return st;
     }
     DecodePartials mine;
