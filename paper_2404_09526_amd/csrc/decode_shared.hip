@@ -3,196 +3,411 @@
 // n times its bytes; here it is read once per group.  The queries of a group are packed rows, (request, query head of the group) pairs of a
 // KV head, and the columns of MFMA tiles:
 //   S^T [keys x columns] = K Q^T,   O^T [128 x columns] += V^T P^T
-// against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row); the requests' own rows are the plain
-// decode's partials; one kernel combines both.
+// against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row).  With few columns the prefix is bound by the
+// memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
+// ranges side by side, and what bounds the one is left over by the other.  A second launch combines the partials of both kinds.
 #include <math.h>
+#include <stdlib.h>
 
 #include "column_tile.h"
 #include "decode_merge.h"
 
 namespace esp {
 
-constexpr int kSharedWaves = 4;
+constexpr int kSharedWaves = 8;
+constexpr int kSharedTile = kColKBytes + kColVBytes;
+constexpr int kSharedHalf = 64 * 1024;
+constexpr int kSharedMost = 4096;                                   // keys of a prefix range: its slots lie in LDS
+constexpr int kSharedOwn = kSharedMost / kSharedWaves;              // keys of an own range, a wavefront's
+constexpr int kSharedLds = 2 * kSharedHalf + kSharedMost * 4;
+// tiles that wavefronts have for themselves lie before the lists; the blocks of the combination, which are larger, may lie on them: it comes last
+static_assert(kSharedWaves * kSharedTile <= 2 * kSharedHalf && kSharedWaves * kColWaveBytes <= kSharedLds, "the wavefronts' tiles and blocks fit");
+// The offset that probabilities are taken against is moved (and the accumulators with it) only where a score lies this far above it, in log2:
+// moved with every new maximum, as the plain decode's, it moves in half of the tiles for some column of the 32.  Probabilities are up to
+// 2^8 then, which changes nothing for their bf16 or the fp32 sums.
+constexpr float kSharedSlack = 8.f;
 
 struct SharedParts { float* acc; float* ml; int32_t range; };
+// The work of the first launch: `prefix` workgroups on the prefix (units (range, KV head), `blocks` column blocks each) and `own` on the requests' own
+// rows, in eights, spread evenly among each other.
+struct SharedWork { int32_t prefix, own, units, blocks; };
 
-__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_prefix_kernel(SharedArgs a, float scale_log2, SharedParts parts) {
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedWaves * kColWaveBytes];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int qi = lane & 31, hi = lane >> 5;
-    const int kvh = blockIdx.y, G = a.Hq / a.Hkv;
-    const RequestRange at = request_range(blockIdx.x, parts.range, a.n_groups, a.prefix_offsets, lane);
-    const int32_t t0 = at.t0, t1 = min(at.t1, a.prefix_total);      // (never past the slot list)
-    const int32_t b0 = a.group_offsets[at.b], n_req = min(min(a.group_offsets[at.b + 1], a.B) - b0, a.max_group);
-    const int32_t n_rows = n_req * G;                                // at most 32 in every group
-    if (t0 >= t1 || n_rows <= 0) return;
-    const int32_t seg = t1 - t0;
-    const int32_t rho = min(qi, n_rows - 1), of = rho / G;
-    const int32_t row = of * a.Hq + kvh * G + (rho - of * G);         // within the group's queries
-
-    const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
-    const char* kbase = a.k_pool + (uint32_t)kvh * (kHeadDim * 2);
-    const char* vbase = a.v_pool + (uint32_t)kvh * (kHeadDim * 2);
-    const uint32_t lds_k = (uint32_t)(uintptr_t)(ESP_LDS unsigned char*)smem + wave * kColWaveBytes, lds_v = lds_k + kColKBytes;
-
-    bf16x8 qf[8];
-    const uint16_t* qp = (const uint16_t*)a.q + ((int64_t)b0 * a.Hq + row) * kHeadDim + 8 * hi;
+// A wavefront on tiles of 32 keys of its own, number `first`, first + step, ...: their rows go to its block of the LDS, the next tile's K as soon
+// as this one's scores are taken, its V as soon as this one's has been read.  list: the slots of all `seg` keys, in LDS (a load of them on the way would
+// be waited for with everything that was asked for before it).
+__device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8], uint32_t lds_k, const char* kbase, const char* vbase, uint32_t row_bytes,
+                                            int first, int step, int32_t seg, const int32_t* list, float scale_log2, int lane) {
+    const int hi = lane >> 5;
+    uint32_t slot[8];
+    auto fetch_k = [&](int i) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        uint4 raw = *(const uint4*)(qp + 16 * t);
-        if (qi >= n_rows) raw = make_uint4(0u, 0u, 0u, 0u);
-        qf[t] = __builtin_bit_cast(bf16x8, raw);
-    }
-    Columns cols;
-    cols.place(lds_k, lane);
-    cols.clear();
-    auto tile_slots = [&](int i) { return a.prefix_slots[t0 + 32 * i + min(qi, min(32, seg - 32 * i) - 1)]; };
-    int32_t slots = 32 * wave < seg ? tile_slots(wave) : 0;
-    for (int i = wave; 32 * i < seg; i += kSharedWaves) {
+        for (int n = 0; n < 8; ++n) slot[n] = (uint32_t)list[min(32 * i + col_row(n, lane), seg - 1)];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) load_to_lds_b128_at_nt(lds_k + 1024 * n, kbase + ((uint64_t)slot[n] * row_bytes + col_k_within(n, lane)));
+    };
+    auto fetch_v = [&] {
+#pragma unroll
+        for (int n = 0; n < 8; ++n) load_to_lds_b128_at_nt(lds_k + kColKBytes + 1024 * n, vbase + ((uint64_t)slot[n] * row_bytes + col_v_within(lane)));
+    };
+    if (32 * first >= seg) return;
+    fetch_k(first);
+    fetch_v();
+    for (int i = first; 32 * i < seg; i += step) {
         const int rows = min(32, seg - 32 * i);
-        uint64_t row_at[8];
-#pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            row_at[n] = (uint64_t)(uint32_t)__shfl(slots, col_row(n, lane)) * row_bytes;
-            load_to_lds_b128_at(lds_k + 1024 * n, kbase + (row_at[n] + col_k_within(n, lane)));
-        }
-#pragma unroll
-        for (int n = 0; n < 8; ++n) load_to_lds_b128_at(lds_v + 1024 * n, vbase + (row_at[n] + col_v_within(lane)));
-        int32_t slots_next = 0;
-        if (32 * (i + kSharedWaves) < seg) slots_next = tile_slots(i + kSharedWaves);
-        wait_vm<8>();                                               // K has landed; V and the next slots may be on their way
+        const bool next = 32 * (i + step) < seg;
+        wait_vm<8>();                                               // K has landed; V may be on its way
         floatx16 sc = cols.scores(qf);
-        if (rows < 32) {
+        if (next) {
+            asm volatile("" :: "v"(sc));                            // K has been read
+            fetch_k(i + step);
+        }
+        if (rows < 32) {                                            // keys past the end are hidden
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (8 * (r >> 2) + 4 * hi + (r & 3) >= rows) sc[r] = -INFINITY;
         }
         Columns::PFrag pf[2];
         cols.weigh(sc, scale_log2, pf);
-        wait_vm<0>();
-        asm volatile("" :: "v"(slots_next));
+        if (next) wait_vm<8>(); else wait_vm<0>();
         cols.accumulate(pf);
-        slots = slots_next;
+        if (next) fetch_v();
     }
-    float out[64 / kSharedWaves], mx, lsum;
-    cols.combine<kSharedWaves>(smem, wave, lane, out, mx, lsum);
-    if (qi >= n_rows) return;
-    const int64_t ph = (int64_t)(at.w + at.b) * a.max_group * a.Hq + row;
-    float* dst = parts.acc + ph * kHeadDim + Columns::first_element<kSharedWaves>(wave, lane);
-#pragma unroll
-    for (int e = 0; e < 64 / kSharedWaves; e += 4) *(float4*)(dst + 2 * e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
-    if (wave == 0 && hi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
 }
 
-// More columns than one tile has: a workgroup of eight wavefronts has COLS tiles of 32 of them, a wavefront one, and the COLS wavefronts that
-// have different columns (a team) share tiles of 32 keys in LDS, so that a row of K and V comes from memory once for 32 COLS columns; the 8 / COLS
-// teams take the tiles in turn.  All teams' tiles are a step; COLS steps are on their way or at work (128 KiB of LDS in every form), and one
-// barrier a step says both that its tiles are there and that the stage of the step before may be filled again.
-constexpr int kWideWaves = 8;
-constexpr int kWideTile = kColKBytes + kColVBytes;
-constexpr int kWideMost = 4096;                                     // keys of a range: its slots lie in LDS
+// Ranges counted from each list's first token on (lists: offsets[b] .. offsets[b + 1]), all whole ones first, then what is left of each list: where
+// range i is, as request_range (esp_common.h) finds it, but 64 N lists at a time, whose offsets are one round trip for both kinds where that is all.
+template <int N>
+__device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int lane) {
+    int32_t s0[N], s1[N];
+#pragma unroll 1
+    for (int rest = 0; rest < 2; ++rest) {
+#pragma unroll 1
+        for (int base = 0; base < B; base += 64 * N) {
+            if (rest == 0 || B > 64 * N) {
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const int b = min(base + 64 * u + lane, B - 1);
+                    s0[u] = offsets[b]; s1[u] = offsets[b + 1];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                if (base + 64 * u >= B) break;
+                const int32_t whole = (uint32_t)max(s1[u] - s0[u], 0) / (uint32_t)range;
+                const int32_t n = base + 64 * u + lane >= B ? 0 : rest ? (s1[u] - s0[u] > whole * range ? 1 : 0) : whole;
+                int32_t upto = n;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int32_t below = __shfl_up(upto, d);
+                    if (lane >= d) upto += below;
+                }
+                const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > i);
+                if (hit) {
+                    const int l = __builtin_ctzll(hit);
+                    const int32_t start = __builtin_amdgcn_readlane(s0[u], l), end = __builtin_amdgcn_readlane(s1[u], l);
+                    const int32_t part = rest ? __builtin_amdgcn_readlane(whole, l) : i - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+                    const int32_t t0 = start + part * range;
+                    return {base + 64 * u + l, t0, t0 + min(range, end - t0), start / range + part};
+                }
+                i -= __builtin_amdgcn_readlane(upto, 63);
+            }
+        }
+    }
+    return {0, 0, 0, 0};                                            // the launch is an upper bound
+}
 
+// The requests' own rows: a wavefront alone on (a range of a request, KV head, up to 32 of its query heads), heads next to each other as in a
+// pool row; its partial goes to the plain decode's slot of that range.
+__device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2, const DecodePartials& mine, int32_t index, unsigned char* smem, int wave, int lane) {
+    const int qi = lane & 31, hi = lane >> 5;
+    const int G = a.Hq / a.Hkv, chunks = (G + 31) / 32;
+    const uint32_t unit = (uint32_t)index * kSharedWaves + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
+    const int kvh = rest / (uint32_t)chunks, g0 = (rest - kvh * chunks) * 32, ng = min(32, G - g0), h0 = kvh * G + g0;
+    const RequestRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, lane);
+    const int32_t seg = min(at.t1, a.total_tokens) - at.t0;         // (never past the slot list)
+    if (seg <= 0) return;
+    int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf) + wave * kSharedOwn;
+    for (int j = lane; j < seg; j += 64) list[j] = a.slot_idx[at.t0 + j];
+    bf16x8 qf[8];
+    const int64_t row = (int64_t)at.b * a.Hq + h0 + min(qi, ng - 1);
+    const uint16_t* qp = (const uint16_t*)a.q + row * kHeadDim + 8 * hi;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) qf[t] = *(const bf16x8*)(qp + 16 * t);
+    asm volatile("" :: "v"(qf[0]), "v"(qf[1]), "v"(qf[2]), "v"(qf[3]), "v"(qf[4]), "v"(qf[5]), "v"(qf[6]), "v"(qf[7]));   // here before the transfers, whose waits count
+    const uint32_t lds_k = (uint32_t)(uintptr_t)(ESP_LDS unsigned char*)smem + wave * kSharedTile;
+    Columns cols;
+    cols.place(lds_k, lane);
+    cols.clear();
+    sweep_tiles(cols, qf, lds_k, a.k_pool + (uint32_t)kvh * (kHeadDim * 2), a.v_pool + (uint32_t)kvh * (kHeadDim * 2), (uint32_t)a.Hkv * (kHeadDim * 2), 0, 1, seg, list,
+                scale_log2, lane);
+    const float l = half_swap_sum(cols.l), l_r = half_swap_sum(cols.l_r), fix = l_r > 0.f ? l / l_r : 0.f;
+    if (qi >= ng) return;
+    const int64_t ph = (int64_t)(at.w + at.b) * a.Hq + h0 + qi;
+    float* dst = const_cast<float*>(mine.acc) + ph * kHeadDim + 4 * hi;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *(float4*)(dst + 32 * db + 2 * r) = make_float4(cols.oacc[db][r] * fix, cols.oacc[db][r + 1] * fix, cols.oacc[db][r + 2] * fix, cols.oacc[db][r + 3] * fix);
+    if (hi == 0) *(float2*)(const_cast<float*>(mine.ml) + ph * 2) = make_float2(cols.m, l);
+}
+
+// The prefix.  A workgroup of eight wavefronts has COLS tiles of 32 columns, a wavefront one, and the COLS wavefronts that have different
+// columns (a team) share tiles of 32 keys in LDS, so that a row of K and V comes from memory once for 32 COLS columns; the 8 / COLS teams take
+// the tiles in turn, all teams' tiles are a step.
+// A step of a wavefront is two phases that take about as long as each other: the scores of its tile become probabilities (vector ALU); then the
+// products, the NEXT tile's scores and this one's V, without a wait, each followed by the LDS read of the operand that takes its place
+// (matrix cores).  The two wavefronts of a SIMD are a phase apart, the barriers between phases keep them so.  K's operands are thus read two steps ahead
+// of the scores, V's one step ahead of their products, and each has a ring of COLS stages (128 KiB together): group j of transfers is V of step j
+// and K of step j + 1.
+// A team of one wavefront shares nothing: it waits for its own rows only (sweep_tiles).
 template <int COLS>
-__global__ __launch_bounds__(kWideWaves * 64, 2) void shared_wide_kernel(SharedArgs a, float scale_log2, SharedParts parts, int32_t units, int32_t col_blocks) {
-    constexpr int TEAMS = kWideWaves / COLS, STAGES = COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: transfers of K, and of V, of a wavefront a step
-    constexpr int kRing = STAGES * TEAMS * kWideTile, kLds = kRing + kWideMost * 4;
-    static_assert(kRing + 1 >= 128 * 1024 && kWideWaves * kColWaveBytes <= kLds, "the blocks of the combination fit");
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[kLds];
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, uint32_t unit, uint32_t cb, bool once,
+                                              unsigned char* smem, int wave, int lane) {
+    constexpr int TEAMS = kSharedWaves / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
     const int team = wave / COLS, ct = wave % COLS;
     const int qi = lane & 31, hi = lane >> 5;
-    // unit: (range, KV head), heads next to each other as in a pool row.  The column blocks of a unit are eight workgroups apart: on one XCD, whose
-    // L2 then has the rows.
-    const uint32_t all = blockIdx.x, eight = all / (8u * col_blocks), rest = all - eight * (8u * col_blocks);
-    const uint32_t unit = eight * 8 + (rest & 7), cb = rest >> 3;
-    if (unit >= (uint32_t)units) return;
     const int kvh = unit % (uint32_t)a.Hkv, G = a.Hq / a.Hkv;
-    const RequestRange at = request_range(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
+    const RequestRange at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
     const int32_t t0 = at.t0, t1 = min(at.t1, a.prefix_total);      // (never past the slot list)
     const int32_t b0 = a.group_offsets[at.b], n_req = min(min(a.group_offsets[at.b + 1], a.B) - b0, a.max_group);
-    const int32_t seg = t1 - t0;
-    if (seg <= 0 || n_req * G <= (int32_t)cb * (32 * COLS)) return;
-    const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = min(32, n_req * G - rho0);   // (columns of this wavefront; none: it only moves tiles)
+    const int32_t seg = t1 - t0, n_all = n_req * G;
+    if (seg <= 0 || n_all <= (int32_t)cb * (32 * COLS)) return;
+    const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = n_all - rho0;   // (columns of this wavefront, up to 32; none: it only moves tiles)
 
-    int32_t* const list = (int32_t*)(smem + kRing);
-    for (int i = threadIdx.x; i < seg; i += kWideWaves * 64) list[i] = a.prefix_slots[t0 + i];
+    int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf);
+    for (int i = threadIdx.x; i < seg; i += kSharedWaves * 64) list[i] = a.prefix_slots[t0 + i];
 
-    const int32_t rho = rho0 + max(min(qi, n_rows - 1), 0), rho_in = min(rho, n_req * G - 1), of = rho_in / G;
-    const int32_t row = of * a.Hq + kvh * G + (rho_in - of * G);      // within the group's queries
+    // row of this column within the group's queries (past the last: the last one's, whose results are not written)
+    const int32_t rho = min(rho0 + qi, n_all - 1), of = rho / G;
+    const int32_t row = of * a.Hq + kvh * G + (rho - of * G);
     bf16x8 qf[8];
     const uint16_t* qp = (const uint16_t*)a.q + ((int64_t)b0 * a.Hq + row) * kHeadDim + 8 * hi;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        uint4 raw = *(const uint4*)(qp + 16 * t);
-        if (qi >= n_rows) raw = make_uint4(0u, 0u, 0u, 0u);
-        qf[t] = __builtin_bit_cast(bf16x8, raw);
-    }
+    for (int t = 0; t < 8; ++t) qf[t] = *(const bf16x8*)(qp + 16 * t);
     asm volatile("" :: "v"(qf[0]), "v"(qf[1]), "v"(qf[2]), "v"(qf[3]), "v"(qf[4]), "v"(qf[5]), "v"(qf[6]), "v"(qf[7]));   // here before the transfers, whose waits count
-    __syncthreads();
 
     const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
     const char* kbase = a.k_pool + (uint32_t)kvh * (kHeadDim * 2);
     const char* vbase = a.v_pool + (uint32_t)kvh * (kHeadDim * 2);
     const uint32_t lds = (uint32_t)(uintptr_t)(ESP_LDS unsigned char*)smem;
-    const int steps = (seg + STEP - 1) / STEP;
-    auto fetch = [&](int i) {
-        const uint32_t to = lds + ((i % STAGES) * TEAMS + team) * kWideTile;
-        uint64_t row_at[MOVES];
-#pragma unroll
-        for (int x = 0; x < MOVES; ++x) {
-            const int n = ct + COLS * x;
-            row_at[x] = (uint64_t)(uint32_t)list[min(i * STEP + team * 32 + col_row(n, lane), seg - 1)] * row_bytes;
-            load_to_lds_b128_at(to + 1024 * n, kbase + (row_at[x] + col_k_within(n, lane)));
-        }
-#pragma unroll
-        for (int x = 0; x < MOVES; ++x) {
-            const int n = ct + COLS * x;
-            load_to_lds_b128_at(to + kColKBytes + 1024 * n, vbase + (row_at[x] + col_v_within(lane)));
-        }
-    };
-    // the transfers of step i have landed: those of up to STAGES - 2 steps after it may be on their way
-    auto landed = [&](int i) {
-        const int after = min(steps - 1 - i, STAGES - 2);
-        if (after <= 0) wait_vm<0>();
-        else if (after == 1) wait_vm<2 * MOVES>();
-        else if (after == 2) wait_vm<4 * MOVES>();
-        else if (after == 3) wait_vm<6 * MOVES>();
-        else if (after == 4) wait_vm<8 * MOVES>();
-        else if (after == 5) wait_vm<10 * MOVES>();
-        else wait_vm<12 * MOVES>();
-    };
-    for (int i = 0; i < STAGES - 1 && i < steps; ++i) fetch(i);
-
     Columns cols;
     cols.clear();
-    for (int i = 0; i < steps; ++i) {
-        landed(i);
-        wg_barrier();
-        if (i + STAGES - 1 < steps) fetch(i + STAGES - 1);
-        const int here = seg - i * STEP - team * 32;                // keys of this tile
-        if (n_rows <= 0 || here <= 0) continue;
-        cols.place(lds + ((i % STAGES) * TEAMS + team) * kWideTile, lane);
-        floatx16 sc = cols.scores(qf);
-        if (here < 32) {
+    __syncthreads();                                                // the list is there
+    if constexpr (COLS == 1) {
+        cols.place(lds + wave * kSharedTile, lane);
+        sweep_tiles(cols, qf, lds + wave * kSharedTile, kbase, vbase, row_bytes, wave, kSharedWaves, seg, list, scale_log2, lane);
+    } else {
+        constexpr int STAGES = COLS, kTile = kColKBytes;            // of K; V's is as large
+        constexpr int kRing = STAGES * TEAMS * kTile;
+        static_assert(2 * kRing == 2 * kSharedHalf, "both rings end where the list begins");
+        const bool late = wave >= kSharedWaves / 2;                 // (wavefronts w and w + 4 are on one SIMD)
+        const int steps = (seg + STEP - 1) / STEP;
+        auto k_tile = [&](int i) { return lds + ((i % STAGES) * TEAMS + team) * kTile; };
+        auto v_tile = [&](int i) { return lds + kRing + ((i % STAGES) * TEAMS + team) * kTile; };
+        // A wavefront's rows of a tile are the same for K and V: slots are looked up a group ahead, and a row's place is kept from K's group to V's.
+        uint32_t slot[MOVES];
+        uint64_t place[MOVES];
+        auto look_up = [&](int i) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
+            for (int x = 0; x < MOVES; ++x) slot[x] = (uint32_t)list[min(i * STEP + team * 32 + col_row(ct + COLS * x, lane), seg - 1)];
+        };
+        auto fetch_k = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < MOVES; ++x) {
+                const int n = ct + COLS * x;
+                place[x] = (uint64_t)slot[x] * row_bytes;
+                const uint32_t to = __builtin_amdgcn_readfirstlane(k_tile(i) + 1024 * n);
+                if (once) load_to_lds_b128_at_nt(to, kbase + (place[x] + col_k_within(n, lane)));
+                else load_to_lds_b128_at(to, kbase + (place[x] + col_k_within(n, lane)));
+            }
+        };
+        auto fetch_v = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < MOVES; ++x) {
+                const uint32_t to = __builtin_amdgcn_readfirstlane(v_tile(i) + 1024 * (ct + COLS * x));
+                if (once) load_to_lds_b128_at_nt(to, vbase + (place[x] + col_v_within(lane)));
+                else load_to_lds_b128_at(to, vbase + (place[x] + col_v_within(lane)));
+            }
+        };
+        auto fetch_group = [&](int j) {
+            if (j < steps) fetch_v(j);
+            if (j + 1 < steps) { fetch_k(j + 1); look_up(j + 2); }
+        };
+        // Group i + 1, of which the products of step i read, has landed: STAGES - 2 groups behind it may be on their way (the last one has no K).
+        auto landed = [&](int i) {
+            if (i + STAGES < steps) { wait_vm<2 * (STAGES - 2) * MOVES>(); return; }
+            constexpr int kMore = COLS > 2 ? MOVES : 0, kEight = COLS == 8 ? MOVES : 0;   // (as many as the stages allow)
+            const int left = steps - 2 - i;
+            if (left <= 0) wait_vm<0>();
+            else if (left == 1) wait_vm<kMore>();
+            else if (left == 2) wait_vm<3 * kMore>();
+            else if (left == 3) wait_vm<5 * kEight>();
+            else if (left == 4) wait_vm<7 * kEight>();
+            else if (left == 5) wait_vm<9 * kEight>();
+            else wait_vm<11 * kEight>();
+        };
+        auto meet = [] {
+            __builtin_amdgcn_sched_barrier(0);
+            wg_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        cols.place(0, lane);                                        // (offsets within a tile; of V behind K's)
+        const uint32_t k_rd = cols.k_rd;
+        bf16x8 kf[8];
+        Columns::VFrag vf[8];
+        auto read_k = [&](uint32_t tile, int t) { kf[t] = *(const ESP_LDS bf16x8*)(uintptr_t)((k_rd ^ (t << 5)) + tile); };
+        auto read_v = [&](uint32_t tile, int p) {
+            const uint32_t vp = cols.v_rd[p & 3] + (tile - kColKBytes + (16 * (p >> 2)) * 256);
+            vf[p].s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ESP_LDS short4_t*)(uintptr_t)(vp));
+            vf[p].s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ESP_LDS short4_t*)(uintptr_t)(vp + 8 * 256));
+        };
+        floatx16 sc;
+        auto zero = [&] {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+        };
+
+        look_up(0);
+        fetch_k(0);
+        look_up(1);
+#pragma unroll 1
+        for (int j = 0; j < STAGES - 1; ++j) fetch_group(j);
+        landed(-1);
+        meet();
+        zero();
+        if (n_rows > 0) {
+#pragma unroll
+            for (int t = 0; t < 8; ++t) read_k(k_tile(0), t);
+#pragma unroll
+            for (int t = 0; t < 8; ++t) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], qf[t], sc, 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < 8; ++t) { read_k(k_tile(1), t); read_v(v_tile(0), t); }
         }
-        Columns::PFrag pf[2];
-        cols.weigh(sc, scale_log2, pf);
-        cols.accumulate(pf);
-    }
-    float out[64 / TEAMS], mx, lsum;
-    __syncthreads();                                                // the ring is read: it may hold the teams' results
-    cols.combine<TEAMS, COLS>(smem + ct * kColWaveBytes, team, lane, out, mx, lsum);
-    if (qi >= n_rows) return;
-    const int64_t ph = (int64_t)(at.w + at.b) * a.max_group * a.Hq + row;
-    float* dst = parts.acc + ph * kHeadDim + Columns::first_element<TEAMS>(team, lane);
+        meet();                                                     // K of steps 0 and 1 and V of step 0 are read
+        fetch_group(STAGES - 1);
+        if (late) { landed(0); meet(); }
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+            Columns::PFrag pf[2];
+            if (n_rows > 0) {
+                const int here = seg - i * STEP - team * 32;
+                if (here < 32) {                                    // keys past the end are hidden
 #pragma unroll
-    for (int e = 0; e < 64 / TEAMS; e += 4) *(float4*)(dst + 2 * e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
-    if (team == 0 && hi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
+                    for (int r = 0; r < 16; ++r)
+                        if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
+                }
+                float top = sc[0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+                top = half_swap_max(top) * scale_log2;
+                if (__builtin_amdgcn_ballot_w64(top > cols.m + kSharedSlack) != 0) {
+                    // (a column that has seen nothing but -inf and NaN stays as it is: exp2(-inf - -inf) must not leak into sums that are zero)
+                    const float to = fmaxf(cols.m, top), alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(cols.m - to);
+                    cols.m = to;
+                    cols.l *= alpha; cols.l_r *= alpha;
+#pragma unroll
+                    for (int db = 0; db < 4; ++db)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) cols.oacc[db][r] *= alpha;
+                }
+                const float sub = cols.m == -INFINITY ? 0.f : cols.m;
+                float sum = 0.f, sum_r = 0.f;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c], scale_log2, -sub));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c + 1], scale_log2, -sub));
+                    sum += p0 + p1;
+                    const uint32_t pk = pack_bf16(p0, p1);
+                    sum_r = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum_r, false);
+                    pf[c >> 2].u[c & 3] = pk;
+                }
+                cols.l += sum; cols.l_r += sum_r;
+            }
+            if (!late) landed(i);
+            meet();
+            // (past the last step there is nothing to read: what is there instead is never used)
+            if (n_rows > 0) {
+                const uint32_t k_next = k_tile(i + 2), v_next = v_tile(i + 1);
+                zero();
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], qf[t], sc, 0, 0, 0);
+                    read_k(k_next, t);
+                    cols.oacc[t & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t].v, pf[t >> 2].v, cols.oacc[t & 3], 0, 0, 0);
+                    read_v(v_next, t);
+                    __builtin_amdgcn_sched_barrier(0);              // (in this order: the chain of the scores beside the sums of V, an operand's place taken over at once)
+                }
+            }
+            // every wavefront is done with the products of the step before this one, and with what they read
+            fetch_group(i + STAGES);
+            if (late) landed(i + 1);
+            meet();
+        }
+        if (!late) meet();
+    }
+    // The wavefronts leave their columns as rows of 128 (and 4 of padding) floats in LDS, maxima and sums behind them; then every wavefront combines
+    // the teams' rows and stores its share of them, 32 lanes a row.  (Stored from the accumulators, 16 bytes of 32 rows at a time, 256 such blocks took 11 us.)
+    constexpr int kPitch = kHeadDim + 4;
+    static_assert(32 * kPitch * 4 <= kColWaveBytes && kSharedWaves * (kColWaveBytes + 32 * 8) <= kSharedLds, "the rows fit");
+    __syncthreads();                                                // the tiles are read
+    {
+        const float l = half_swap_sum(cols.l), l_r = half_swap_sum(cols.l_r), fix = l_r > 0.f ? l / l_r : 0.f;   // (the rounded probabilities were multiplied)
+        float* mine = (float*)(smem + wave * kColWaveBytes) + qi * kPitch + 4 * hi;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(float4*)(mine + 32 * db + 2 * r) = make_float4(cols.oacc[db][r] * fix, cols.oacc[db][r + 1] * fix, cols.oacc[db][r + 2] * fix, cols.oacc[db][r + 3] * fix);
+        if (hi == 0) ((float2*)(smem + kSharedWaves * kColWaveBytes))[wave * 32 + qi] = make_float2(cols.m, l);
+    }
+    __syncthreads();
+    const int64_t slot = (int64_t)(at.w + at.b) * a.max_group * a.Hq;
+#pragma unroll 1
+    for (int i = 0; i < 2 * COLS; ++i) {
+        const int in = (wave * 2 * COLS + i) * 2 + hi;              // of the workgroup's 32 COLS columns
+        const int32_t col = cb * (32 * COLS) + in;
+        if (col >= n_all) continue;
+        const int w0 = in >> 5, at_row = in & 31;                   // team t's are those of wavefront w0 + COLS t
+        float2 ml[TEAMS];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < TEAMS; ++t) {
+            ml[t] = ((const float2*)(smem + kSharedWaves * kColWaveBytes))[(w0 + COLS * t) * 32 + at_row];
+            mx = fmaxf(mx, ml[t].x);
+        }
+        float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+        float lsum = 0.f;
+#pragma unroll
+        for (int t = 0; t < TEAMS; ++t) {
+            const float4 x = *(const float4*)((const float*)(smem + (w0 + COLS * t) * kColWaveBytes) + at_row * kPitch + 4 * qi);
+            // a team that saw no key (sum 0) has nothing to add; a NaN sum shows in l * c
+            const float c = ml[t].y > 0.f ? __builtin_amdgcn_exp2f(ml[t].x - mx) : 0.f;
+            lsum += ml[t].y * c;
+            out.x += x.x * c; out.y += x.y * c; out.z += x.z * c; out.w += x.w * c;
+        }
+        const int32_t req = col / G;
+        const int64_t ph = slot + req * a.Hq + kvh * G + (col - req * G);
+        ((float4*)(parts.acc + ph * kHeadDim))[qi] = out;
+        if (qi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
+    }
+}
+
+template <int COLS>
+__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, DecodePartials mine, SharedWork work) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedLds];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // the eight that this workgroup is of, and how many before it are the prefix's: the workgroups of an eight lie on all XCDs in turn
+    const uint32_t eight = blockIdx.x >> 3, of = blockIdx.x & 7, prefix = work.prefix >> 3, all = (work.prefix + work.own) >> 3;
+    const uint32_t before = (uint64_t)eight * prefix / all, after = (uint64_t)(eight + 1) * prefix / all;
+    if (after > before) {
+        // The column blocks of a unit are in eights that follow each other: on one XCD, whose L2 then has the rows.
+        const uint32_t unit = before / work.blocks * 8 + of, cb = before % work.blocks;
+        if (unit < (uint32_t)work.units) shared_prefix<COLS>(a, scale_log2, parts, unit, cb, work.blocks == 1, smem, wave, lane);
+    } else {
+        shared_own(a, scale_log2, mine, (eight - before) * 8 + of, smem, wave, lane);
+    }
 }
 
 // Combination, as the plain decode's (decode.hip): groups of 32 lanes take a pair's partials in turn, four at a time, first those of the
@@ -269,74 +484,83 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
     if (lane == 0) a.LSE[pair] = Lt == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(Lt)) * kLn2;
 }
 
-// Ranges of the prefix lists, which kernel has them, and the partials' slots.
-struct SharedPlan { int32_t cols, range; };                         // cols: column tiles of a workgroup; 1: the kernel for one
-static SharedPlan shared_plan(int32_t prefix_total, int32_t max_group, int32_t Hq, int32_t Hkv) {
-    const int64_t rows = (int64_t)max_group * (Hq / Hkv);
-    if (rows <= 32) return {1, decode_range(prefix_total, kSharedWaves * 32, 1, Hkv, 1, 1 << 20)};
-    const int32_t cols = rows <= 64 ? 2 : rows <= 128 ? 4 : 8, step = 32 * (kWideWaves / cols);
+// The ranges of both kinds, and the workgroups that they are.
+struct SharedPlan {
+    int32_t cols, range, own_range;                                 // column tiles of a workgroup; keys of a range
+    size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
+    int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
+};
+static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    SharedPlan p = {};
+    const int64_t G = Hq / Hkv, rows = max_group * G, chunks = (G + 31) / 32;
+    p.cols = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    p.blocks = (rows + 32 * p.cols - 1) / (32 * p.cols);
+    const int64_t step = 32 * (kSharedWaves / p.cols);
     // One workgroup a CU.  Of the ranges that fill 1 .. 16 rounds of them the one whose rounds, each with a start, an end (its partial, written and
     // read) and its steps, take the least time.
     constexpr int64_t kResident = 256;
-    const double start = 6 + 0.04 * 32 * cols, per_step = 0.63 * (kWideWaves / cols);
-    const int64_t steps = ((int64_t)prefix_total + step - 1) / step, units = Hkv * ((rows + 32 * cols - 1) / (32 * cols));
+    const double start = 6 + 0.04 * 32 * p.cols, per_step = 0.63 * (kSharedWaves / p.cols);
+    const int64_t steps = ((int64_t)prefix_total + step - 1) / step, wide = Hkv * p.blocks;
     int64_t best = 1;
     double best_us = 0;
     for (int64_t rounds = 1; rounds <= 16; ++rounds) {
-        const int64_t fit = rounds * kResident / units;
+        const int64_t fit = rounds * kResident / wide;
         int64_t take = fit > 0 ? (steps + fit - 1) / fit : steps;
-        if (take > kWideMost / step) take = kWideMost / step;
-        const int64_t wgs = (steps + take - 1) / take * units;
+        if (take > kSharedMost / step) take = kSharedMost / step;
+        if (take < 1) take = 1;
+        const int64_t wgs = (steps + take - 1) / take * wide;
         const double us = (double)((wgs + kResident - 1) / kResident) * (start + per_step * (double)take);
         if (rounds == 1 || us < best_us) { best = take; best_us = us; }
     }
-    return {cols, (int32_t)(best * step)};
+    if (getenv("XR")) best = atoi(getenv("XR")) / step; if (best < 1) best = 1; if (best > kSharedMost / step) best = kSharedMost / step;
+    p.range = (int32_t)(best * step);
+    p.slots = (size_t)(prefix_total / p.range) + n_groups;
+    p.units = (int64_t)p.slots * Hkv;
+    // a wavefront's range: what there is for each of those that the chip holds, but not so much that the last ones are long waited for
+    int64_t own = ((int64_t)total_tokens * Hkv * chunks / (kResident * kSharedWaves) + 31) / 32 * 32;
+    own = own < 32 ? 32 : own > kSharedOwn ? kSharedOwn : own;
+    if (getenv("XO")) own = atoi(getenv("XO"));
+    p.own_range = (int32_t)own;
+    const int64_t ranges = total_tokens / own + B;                  // (of requests of any lengths)
+    p.own_slots = (size_t)ranges;
+    p.own = total_tokens == 0 ? 0 : (ranges * Hkv * chunks + kSharedWaves - 1) / kSharedWaves;
+    return p;
 }
-static size_t shared_slots(int32_t n_groups, int32_t prefix_total, int32_t range) { return prefix_total > 0 ? (size_t)(prefix_total / range) + n_groups : 0; }
-static size_t shared_prefix_bytes(int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t Hq, int32_t Hkv) {
-    if (prefix_total <= 0) return 0;
-    const size_t slots = shared_slots(n_groups, prefix_total, shared_plan(prefix_total, max_group, Hq, Hkv).range);
-    return (slots * max_group * Hq * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256;
-}
+static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
                                      int32_t Hq, int32_t Hkv) {
     (void)max_prefix;
-    return shared_prefix_bytes(n_groups, prefix_total, max_group, Hq, Hkv) + decode_workspace_bytes(B, total_tokens, Hq, Hkv);
+    if (prefix_total == 0 || max_group == 0) return decode_workspace_bytes(B, total_tokens, Hq, Hkv);
+    const SharedPlan p = shared_plan(B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
+    return partials_bytes(p.slots, (int64_t)max_group * Hq) + partials_bytes(p.own_slots, Hq);
 }
 
 esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_t stream) {
+    if (a.prefix_total == 0 || a.max_group == 0)
+        return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
+                             workspace, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream);
     if ((int64_t)a.B * a.Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode (shared): too many rows for one launch");
-    const int32_t pairs = a.B * a.Hq, G = a.Hq / a.Hkv;
-    SharedParts parts = {(float*)workspace, nullptr, 1};
-    char* mine_at = (char*)workspace;
-    int64_t most = 0;                                               // partials of a pair
-    if (a.prefix_total > 0 && a.max_group > 0) {
-        const SharedPlan plan = shared_plan(a.prefix_total, a.max_group, a.Hq, a.Hkv);
-        parts.range = plan.range;
-        const size_t slots = shared_slots(a.n_groups, a.prefix_total, parts.range);
-        parts.ml = parts.acc + slots * a.max_group * a.Hq * kHeadDim;
-        mine_at += shared_prefix_bytes(a.n_groups, a.prefix_total, a.max_group, a.Hq, a.Hkv);
-        most = a.max_prefix / parts.range + 1;
-        const int64_t tiles = ((int64_t)a.max_group * G + 31) / 32, blocks = (tiles + plan.cols - 1) / plan.cols, units = (int64_t)slots * a.Hkv;
-        if (a.Hkv > 65535 || blocks * ((units + 7) / 8 * 8) > UINT32_MAX / (kWideWaves * 64))
-            return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
-        const float sl2 = a.softmax_scale * kLog2e;
-#define ESP_WIDE_LAUNCH(COLS)                                                                                                               \
-    hipLaunchKernelGGL(shared_wide_kernel<COLS>, dim3((unsigned)((units + 7) / 8 * 8 * blocks)), dim3(kWideWaves * 64), 0, stream, a, sl2, parts, \
-                       (int32_t)units, (int32_t)blocks)
-        if (plan.cols == 1) hipLaunchKernelGGL(shared_prefix_kernel, dim3((unsigned)slots, a.Hkv), dim3(kSharedWaves * 64), 0, stream, a, sl2, parts);
-        else if (plan.cols == 2) ESP_WIDE_LAUNCH(2);
-        else if (plan.cols == 4) ESP_WIDE_LAUNCH(4);
-        else ESP_WIDE_LAUNCH(8);
-#undef ESP_WIDE_LAUNCH
-        const esp_status st = check_launch(plan.cols == 1 ? "shared_prefix_kernel" : "shared_wide_kernel");
-        if (st != ESP_OK) return st;
-    }
-    DecodePartials mine;
-    const esp_status st = launch_decode_partials(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv,
-                                                 a.softmax_scale, mine_at, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream, &mine);
+    const int32_t pairs = a.B * a.Hq;
+    const SharedPlan p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
+    const int64_t prefix = (p.units + 7) / 8 * 8 * p.blocks, own = (p.own + 7) / 8 * 8;
+    if (prefix + own > (int64_t)(UINT32_MAX / (kSharedWaves * 64)) || p.units > INT32_MAX / 2)
+        return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
+    float* const acc = (float*)workspace;
+    const SharedParts parts = {acc, acc + p.slots * a.max_group * a.Hq * kHeadDim, p.range};
+    float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
+    const DecodePartials mine = {p.own_range, -1, own_acc, own_acc + p.own_slots * a.Hq * kHeadDim};
+    const SharedWork work = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks};
+#define ESP_SHARED_LAUNCH(COLS)                                                                                                       \
+    hipLaunchKernelGGL(shared_partial_kernel<COLS>, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, \
+                       parts, mine, work)
+    if (p.cols == 1) ESP_SHARED_LAUNCH(1);
+    else if (p.cols == 2) ESP_SHARED_LAUNCH(2);
+    else if (p.cols == 4) ESP_SHARED_LAUNCH(4);
+    else ESP_SHARED_LAUNCH(8);
+#undef ESP_SHARED_LAUNCH
+    const esp_status st = check_launch("shared_partial_kernel");
     if (st != ESP_OK) return st;
-    most += a.max_len / mine.range + 2;
+    const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair
 #define ESP_COMBINE_LAUNCH(GROUPS)                                                                                                          \
     hipLaunchKernelGGL((shared_combine_kernel<GROUPS>), row_grid(((int64_t)pairs + 8 / GROUPS - 1) / (8 / GROUPS)), dim3(256), 0, stream, a, pairs, parts, mine)
     if (most <= 32) ESP_COMBINE_LAUNCH(2);
