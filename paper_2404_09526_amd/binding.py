@@ -128,7 +128,7 @@ lib = _load()
 
 class _PythonAlone:
     """In place of the native argument checks where they are not built for this torch and Python: every call goes through the Python ones."""
-    kv_append = decode = prefill = merge = staticmethod(lambda *args: None)
+    kv_append = decode = prefill = merge = decode_shared = rotate = extend = slots = staticmethod(lambda *args: None)
 
 
 def _load_marshal():
@@ -139,9 +139,10 @@ def _load_marshal():
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     at = lambda f: ctypes.cast(f, ctypes.c_void_p).value
-    m.bind(_stream, *(at(f) for f in (lib.esp_kv_append, lib.esp_partial_attn_decode, lib.esp_partial_attn_decode_merge,
-                                      lib.esp_partial_attn_prefill, lib.esp_partial_attn_prefill_f32, lib.esp_merge_partials,
-                                      lib.esp_merge_partials_f32)))
+    m.bind(_stream, _device, *(at(f) for f in (
+        lib.esp_kv_append, lib.esp_partial_attn_decode, lib.esp_partial_attn_decode_merge, lib.esp_partial_attn_prefill, lib.esp_partial_attn_prefill_f32,
+        lib.esp_merge_partials, lib.esp_merge_partials_f32, lib.esp_partial_attn_decode_shared, lib.esp_qk_norm_rope_append, lib.esp_extend_block_table,
+        lib.esp_build_slots)))
     return m
 
 
@@ -193,6 +194,10 @@ def _scratch(t: torch.Tensor) -> torch.Tensor:
 def _stream():
     """The current stream of the current device (asked for after a tensor on a device was seen: the runtime is up)."""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _device() -> int:
+    return torch._C._cuda_getDevice()
 
 
 # The checks of the calls below once more in native code (csrc/marshal.cpp): a function of it makes the call and returns its status where
@@ -438,7 +443,7 @@ def _int32(x, name: str) -> int:
 
 def _one_device(*tensors) -> None:
     """All of a call's tensors on the device that is current, whose stream it goes to."""
-    here = torch._C._cuda_getDevice()
+    here = _device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
@@ -454,6 +459,11 @@ def esp_partial_attn_decode_shared(q, k_pool, v_pool, prefix_slots, prefix_offse
     pool rows prefix_slots[prefix_offsets[g] .. prefix_offsets[g+1]) of its group and its own, slot_idx[seq_offsets[b] .. seq_offsets[b+1]).
     A group's prefix is read once.  q [B,Hq,D] bf16, pools [S,Hkv,D] bf16, lists and offsets int32; max_prefix, max_group, max_len: bounds of a
     prefix's tokens, a group's requests and a request's own tokens.  Returns (O bf16 [B,Hq,D], LSE fp32 [B,Hq])."""
+    status = _marshal.decode_shared(q, k_pool, v_pool, prefix_slots, prefix_offsets, group_offsets, max_prefix, max_group, slot_idx, seq_offsets,
+                                    max_len, softmax_scale, O, LSE, workspace)
+    if status is not None:
+        _check(status)
+        return O, LSE
     _dev(q, torch.bfloat16, "q"); _dev(k_pool, torch.bfloat16, "k_pool"); _dev(v_pool, torch.bfloat16, "v_pool")
     for t, name in ((prefix_slots, "prefix_slots"), (prefix_offsets, "prefix_offsets"), (group_offsets, "group_offsets"), (slot_idx, "slot_idx"),
                     (seq_offsets, "seq_offsets")):
@@ -506,6 +516,10 @@ def esp_qk_norm_rope_append(q, k, v, q_pos=None, inv_freq=None, q_weight=None, k
     """Norm (weights bf16 [D], where given) and rotation (by q_pos int32 [T] times inv_freq fp32 [rot/2], where given) of new queries q [T,Hq,D]
     and keys k [T,Hkv,D], and the append of k and v to the pool rows slot_idx (where given; a slot outside the pool: not kept).  q, k, v and q_out may be
     parts of one projection's rows; q_out may be q.  k_out, v_out: dense rows, written where given.  Returns (q_out, k_out, v_out)."""
+    status = _marshal.rotate(q, k, v, q_pos, inv_freq, q_weight, k_weight, eps, interleaved, slot_idx, k_pool, v_pool, q_out, k_out, v_out)
+    if status is not None:
+        _check(status)
+        return q_out, k_out, v_out
     T, Hq, D, q_stride = _heads(q, "q")
     Tk, Hkv, Dk, k_stride = _heads(k, "k")
     Tv, Hv, Dv, v_stride = _heads(v, "v")
@@ -572,6 +586,10 @@ def esp_extend_block_table(block_table, free_pages, old_lens, new_lens, page, re
     """Gives the requests the pages that their tokens old_lens[b] .. new_lens[b] - 1 need, from free_pages on, in block_table int32 [rows, pages]
     (in place; request b is row req_row[b], or row b).  Entries that free_pages is too short for become -1.  Returns pages_taken int32
     [B+1]: request b got free_pages[pages_taken[b] .. pages_taken[b+1])."""
+    status = _marshal.extend(block_table, free_pages, old_lens, new_lens, page, req_row, pages_taken)
+    if status is not None:
+        _check(status)
+        return pages_taken
     B, rows, width = _table(block_table, old_lens, req_row, "old_lens")
     _dev(new_lens, torch.int32, "new_lens"); _dev(free_pages, torch.int32, "free_pages")
     if new_lens.shape != (B,) or free_pages.dim() != 1:
@@ -590,6 +608,11 @@ def esp_build_slots(block_table, lens, page, first_token=None, req_row=None, kee
     """The slots of tokens first_token[b] (or 0) .. lens[b] - 1 of the requests, one request after another; with keep_last > 0 of those only
     the last keep_last and the first keep_first of the request.  The list is written to slot_idx (all of it is room), or to a new one of `capacity`
     entries; token_pos, where given, receives pos_first + pos_stride * token.  Returns (seq_offsets int32 [B+1], slot_idx, token_pos)."""
+    status = _marshal.slots(block_table, lens, page, first_token, req_row, keep_first, keep_last, pos_first, pos_stride, capacity, seq_offsets, slot_idx,
+                            token_pos)
+    if status is not None:
+        _check(status)
+        return seq_offsets, slot_idx, token_pos
     B, rows, width = _table(block_table, lens, req_row, "lens")
     if first_token is not None:
         _dev(first_token, torch.int32, "first_token")

@@ -8,6 +8,7 @@
 // ranges side by side, and what bounds the one is left over by the other.  A second launch combines the partials of both kinds.
 #include <math.h>
 #include <stdlib.h>
+#include <stdio.h>
 
 #include "column_tile.h"
 #include "decode_merge.h"
@@ -161,18 +162,17 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
 // of the scores, V's one step ahead of their products, and each has a ring of COLS stages (128 KiB together): group j of transfers is V of step j
 // and K of step j + 1.
 // A team of one wavefront shares nothing: it waits for its own rows only (sweep_tiles).
+struct PrefixPart { RequestRange at; int32_t b0, seg, n_all, kvh; };  // a range of group at.b's prefix: its keys, the group's first request and packed rows
 template <int COLS>
-__device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, uint32_t unit, uint32_t cb, bool once,
-                                              unsigned char* smem, int wave, int lane) {
+__device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, const PrefixPart& part, uint32_t cb, unsigned char* smem,
+                                              int wave, int lane) {
     constexpr int TEAMS = kSharedWaves / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
     const int team = wave / COLS, ct = wave % COLS;
     const int qi = lane & 31, hi = lane >> 5;
-    const int kvh = unit % (uint32_t)a.Hkv, G = a.Hq / a.Hkv;
-    const RequestRange at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
-    const int32_t t0 = at.t0, t1 = min(at.t1, a.prefix_total);      // (never past the slot list)
-    const int32_t b0 = a.group_offsets[at.b], n_req = min(min(a.group_offsets[at.b + 1], a.B) - b0, a.max_group);
-    const int32_t seg = t1 - t0, n_all = n_req * G;
-    if (seg <= 0 || n_all <= (int32_t)cb * (32 * COLS)) return;
+    const RequestRange& at = part.at;
+    const int32_t t0 = at.t0, b0 = part.b0, seg = part.seg, n_all = part.n_all, kvh = part.kvh, G = a.Hq / a.Hkv;
+    if (n_all <= (int32_t)cb * (32 * COLS)) return;
+    const bool once = n_all <= 32 * COLS;                           // the only workgroup on these rows
     const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = n_all - rho0;   // (columns of this wavefront, up to 32; none: it only moves tiles)
 
     int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf);
@@ -393,7 +393,9 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
     }
 }
 
-template <int COLS>
+// Column tiles of a workgroup on the prefix of a group with so many packed rows.
+__host__ __device__ __forceinline__ int shared_cols(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
+
 __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, DecodePartials mine, SharedWork work) {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedLds];
     const int lane = threadIdx.x & 63;
@@ -401,12 +403,26 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(Sh
     // the eight that this workgroup is of, and how many before it are the prefix's: the workgroups of an eight lie on all XCDs in turn
     const uint32_t eight = blockIdx.x >> 3, of = blockIdx.x & 7, prefix = work.prefix >> 3, all = (work.prefix + work.own) >> 3;
     const uint32_t before = (uint64_t)eight * prefix / all, after = (uint64_t)(eight + 1) * prefix / all;
-    if (after > before) {
-        // The column blocks of a unit are in eights that follow each other: on one XCD, whose L2 then has the rows.
-        const uint32_t unit = before / work.blocks * 8 + of, cb = before % work.blocks;
-        if (unit < (uint32_t)work.units) shared_prefix<COLS>(a, scale_log2, parts, unit, cb, work.blocks == 1, smem, wave, lane);
-    } else {
+    if (after == before) {
         shared_own(a, scale_log2, mine, (eight - before) * 8 + of, smem, wave, lane);
+        return;
+    }
+    // Unit: (range, KV head), heads next to each other as in a pool row.  The column blocks of a unit are in eights that follow each other: on one
+    // XCD, whose L2 then has the rows.
+    const uint32_t unit = before / work.blocks * 8 + of, cb = before % work.blocks;
+    if (unit >= (uint32_t)work.units) return;
+    PrefixPart part;
+    part.kvh = unit % (uint32_t)a.Hkv;
+    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
+    part.b0 = a.group_offsets[part.at.b];
+    part.n_all = min(min(a.group_offsets[part.at.b + 1], a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
+    part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
+    if (part.seg <= 0 || part.n_all <= 0) return;
+    switch (shared_cols(part.n_all)) {
+        case 1: shared_prefix<1>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 2: shared_prefix<2>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 4: shared_prefix<4>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        default: shared_prefix<8>(a, scale_log2, parts, part, cb, smem, wave, lane);
     }
 }
 
@@ -486,44 +502,58 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
 
 // The ranges of both kinds, and the workgroups that they are.
 struct SharedPlan {
-    int32_t cols, range, own_range;                                 // column tiles of a workgroup; keys of a range
+    int32_t cols, range, own_range;                                 // column tiles of a workgroup on the largest group's prefix; keys of a range
     size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
 };
+// One workgroup a CU, whichever kind.  A workgroup on the prefix takes a start, its steps, and an end whose partial is written and read at the memory's
+// rate; one on own rows a start and, when the memory is not what it waits for, 2.5 us for each 32 keys of its longest wavefront.  Own ranges first: the
+// least of what all of them take and a third of the longest; then of the prefix' possible ranges the one whose rounds, alone, or whose share of the chip's time
+// beside the own ranges, is the least.
 static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 2.5;
+    struct Times { double start, step; };
+    constexpr Times kTimes[4] = {{7, 5.3}, {8, 2.9}, {9, 1.3}, {9, 1.15}};   // us, of a workgroup with 1, 2, 4, 8 column tiles
     SharedPlan p = {};
     const int64_t G = Hq / Hkv, rows = max_group * G, chunks = (G + 31) / 32;
-    p.cols = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    p.cols = shared_cols(rows);
+    const int kind = __builtin_ctz(p.cols);
     p.blocks = (rows + 32 * p.cols - 1) / (32 * p.cols);
-    const int64_t step = 32 * (kSharedWaves / p.cols);
-    // One workgroup a CU.  Of the ranges that fill 1 .. 16 rounds of them the one whose rounds, each with a start, an end (its partial, written and
-    // read) and its steps, take the least time.
-    constexpr int64_t kResident = 256;
-    const double start = 6 + 0.04 * 32 * p.cols, per_step = 0.63 * (kSharedWaves / p.cols);
-    const int64_t steps = ((int64_t)prefix_total + step - 1) / step, wide = Hkv * p.blocks;
-    int64_t best = 1;
+
+    double own_us = 0;
+    auto own_wgs = [&](int64_t range) { return ((total_tokens / range + B) * Hkv * chunks + kSharedWaves - 1) / kSharedWaves; };
+    p.own_range = 32;
+    if (total_tokens > 0) {
+        const double tiles = (double)total_tokens / 32 * Hkv * chunks / kSharedWaves;
+        for (int32_t range = 64; range <= kSharedOwn; range += range < 256 ? 64 : 128) {
+            const double us = ((double)own_wgs(range) * kOwnStart + tiles * kOwnTile) / kCus + 0.35 * (kOwnStart + kOwnTile * range / 32);
+            if (range == 64 || us < own_us) { own_us = us; p.own_range = range; }
+        }
+        p.own = own_wgs(p.own_range);
+    }
+    p.own_slots = (size_t)(total_tokens / p.own_range + B);         // (of requests of any lengths)
+
+    const int64_t step = 32 * (kSharedWaves / p.cols), steps = ((int64_t)prefix_total + step - 1) / step, wide = Hkv * p.blocks;
+    const double partial_us = p.cols * 0.009;
     double best_us = 0;
-    for (int64_t rounds = 1; rounds <= 16; ++rounds) {
-        const int64_t fit = rounds * kResident / wide;
-        int64_t take = fit > 0 ? (steps + fit - 1) / fit : steps;
+    int64_t best = 1;
+    auto consider = [&](int64_t ranges) {
+        int64_t take = ranges < 1 ? steps : (steps + ranges - 1) / ranges;
         if (take > kSharedMost / step) take = kSharedMost / step;
         if (take < 1) take = 1;
-        const int64_t wgs = (steps + take - 1) / take * wide;
-        const double us = (double)((wgs + kResident - 1) / kResident) * (start + per_step * (double)take);
-        if (rounds == 1 || us < best_us) { best = take; best_us = us; }
-    }
+        const double wgs = (double)((steps + take - 1) / take + n_groups - 1) * wide, one = kTimes[kind].start + kTimes[kind].step * take;
+        const double alone = ceil(wgs / kCus) * one, beside = (wgs * one) / kCus + own_us + 0.35 * one;
+        const double us = (own_us < 0.5 * one ? alone + own_us : beside) + wgs * partial_us;
+        if (best_us == 0 || us < best_us) { best_us = us; best = take; }
+    };
+    for (int64_t ranges = 1; ranges <= steps && ranges * wide <= 8192; ranges += 1 + ranges / 6) consider(ranges);
+    for (int64_t rounds = 1; rounds <= 8; ++rounds) consider(rounds * (int64_t)kCus / wide - (n_groups - 1));
     if (getenv("XR")) best = atoi(getenv("XR")) / step; if (best < 1) best = 1; if (best > kSharedMost / step) best = kSharedMost / step;
+    if (getenv("XO") && total_tokens > 0) { p.own_range = atoi(getenv("XO")); p.own = own_wgs(p.own_range); p.own_slots = (size_t)(total_tokens / p.own_range + B); }
     p.range = (int32_t)(best * step);
     p.slots = (size_t)(prefix_total / p.range) + n_groups;
     p.units = (int64_t)p.slots * Hkv;
-    // a wavefront's range: what there is for each of those that the chip holds, but not so much that the last ones are long waited for
-    int64_t own = ((int64_t)total_tokens * Hkv * chunks / (kResident * kSharedWaves) + 31) / 32 * 32;
-    own = own < 32 ? 32 : own > kSharedOwn ? kSharedOwn : own;
-    if (getenv("XO")) own = atoi(getenv("XO"));
-    p.own_range = (int32_t)own;
-    const int64_t ranges = total_tokens / own + B;                  // (of requests of any lengths)
-    p.own_slots = (size_t)ranges;
-    p.own = total_tokens == 0 ? 0 : (ranges * Hkv * chunks + kSharedWaves - 1) / kSharedWaves;
+    if (getenv("XV")) printf("cols %d range %d own %d wgs %ld + %ld est %.1f (own %.1f)\n", p.cols, p.range, p.own_range, (long)(p.units * p.blocks), (long)p.own, best_us, own_us);
     return p;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
@@ -550,14 +580,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
     const DecodePartials mine = {p.own_range, -1, own_acc, own_acc + p.own_slots * a.Hq * kHeadDim};
     const SharedWork work = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks};
-#define ESP_SHARED_LAUNCH(COLS)                                                                                                       \
-    hipLaunchKernelGGL(shared_partial_kernel<COLS>, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, \
-                       parts, mine, work)
-    if (p.cols == 1) ESP_SHARED_LAUNCH(1);
-    else if (p.cols == 2) ESP_SHARED_LAUNCH(2);
-    else if (p.cols == 4) ESP_SHARED_LAUNCH(4);
-    else ESP_SHARED_LAUNCH(8);
-#undef ESP_SHARED_LAUNCH
+    hipLaunchKernelGGL(shared_partial_kernel, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
     const esp_status st = check_launch("shared_partial_kernel");
     if (st != ESP_OK) return st;
     const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair

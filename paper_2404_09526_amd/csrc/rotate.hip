@@ -11,6 +11,7 @@
 namespace esp {
 
 constexpr int kRotThreads = 256;
+constexpr int kRotWaves = 4096;                   // that a call asks for where it can: 16 a CU
 
 // Sine and cosine of the angle pos * inv_freq.  In turns, and reduced to half a turn, in 64 bits: at position 2^20 an angle in 32 bits would be off by a
 // tenth of a radian.
@@ -93,8 +94,12 @@ __global__ __launch_bounds__(kRotThreads) void rotate_kernel(RotateArgs a) {
 esp_status launch_rotate(RotateArgs a, int32_t neighbours, hipStream_t stream) {
     const int64_t heads = (int64_t)a.Hq + 2 * (int64_t)a.Hkv;
     if (heads > INT32_MAX / 2) return fail(ESP_ERR_UNSUPPORTED, "norm and rotation: too many heads");
-    a.part_heads = (int32_t)((heads + 3) / 4 * 4);
-    a.parts = 1;
+    // A token's heads by one wavefront, four at a time, as long as there are tokens enough; by several, of which each takes sine and cosine for
+    // itself, where it is a chain of loads: 64 tokens, 32 / 8 heads, 12.0 us with one, XXX with twelve.
+    const int64_t fours = (heads + 3) / 4, parts = a.T > 0 ? kRotWaves / a.T : 1;
+    a.parts = (int32_t)(parts < 1 ? 1 : parts > fours ? fours : parts);
+    a.part_heads = (int32_t)((fours + a.parts - 1) / a.parts * 4);
+    a.parts = (int32_t)((fours * 4 + a.part_heads - 1) / a.part_heads);
     const int64_t blocks = (a.T * (int64_t)a.parts + kRotThreads / 64 - 1) / (kRotThreads / 64);
     if (blocks > kGridMost) return fail(ESP_ERR_INVALID_ARG, "norm and rotation: too many rows for one launch");
     if (neighbours) hipLaunchKernelGGL(rotate_kernel<true>, row_grid(blocks), dim3(kRotThreads), 0, stream, a);

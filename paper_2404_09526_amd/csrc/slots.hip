@@ -12,7 +12,9 @@ namespace esp {
 
 constexpr int kSlotThreads = 256;
 constexpr int kSlotRequests = 1024;               // of a round: four a thread
-constexpr int kSlotChunk = kSlotThreads * 4;      // elements of a workgroup at a time: four a thread, next to each other
+constexpr int kSlotMost = 1536;                   // workgroups: as many as fit the chip at once
+
+struct Int4 { int32_t x, y, z, w; };               // 16 bytes that need not lie on 16
 
 __device__ __forceinline__ int32_t clip32(int64_t x, int32_t most) { return (int32_t)(x < most ? x : most); }
 
@@ -87,16 +89,31 @@ __global__ __launch_bounds__(kSlotThreads) void extend_table_kernel(const int32_
         if (blockIdx.x == 0)
             for (int i = threadIdx.x; i <= n; i += kSlotThreads) taken[r0 + i] = off[i];
         const int32_t first = off[0], end = off[n];
-        // chunk c of the elements is workgroup c % gridDim.x's, whatever round it falls into
-        const int64_t c0 = first / kSlotChunk, turn = ((int64_t)blockIdx.x - c0 % gridDim.x + gridDim.x) % gridDim.x;
-        for (int64_t c = c0 + turn; c * kSlotChunk < end; c += gridDim.x) {
+        // a thread's elements, and the workgroup's chunk of them: chunk c is workgroup c's, c + gridDim.x's, ...
+        const int per = end - first <= kSlotThreads * (int64_t)gridDim.x ? 1 : 4, chunk = kSlotThreads * per;
+        for (int64_t c = first / chunk + blockIdx.x; c * chunk < end; c += gridDim.x) {
+            // four elements next to each other: one search, and where they are one request's whole pieces of 16 bytes
+            const int64_t j0 = c * chunk + per * (int64_t)threadIdx.x;
+            if (j0 + per <= first || j0 >= end) continue;
+            int i = find_request(off, n, (int32_t)max(j0, (int64_t)first));
+            if (per == 4 && j0 >= first && j0 + 4 <= off[i + 1] && j0 + 4 <= n_free) {
+                *(Int4*)(table + ((int64_t)at[i].x * width + at[i].y + ((int32_t)j0 - off[i]))) = *(const Int4*)(free_pages + j0);
+                continue;
+            }
+            int32_t page_no[4];                                     // all loads before the first store: one round trip
+            int64_t to[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t j = c * kSlotChunk + u * kSlotThreads + threadIdx.x;
-                if (j < first || j >= end) continue;
-                const int i = find_request(off, n, (int32_t)j);
-                table[(int64_t)at[i].x * width + at[i].y + ((int32_t)j - off[i])] = j < n_free ? free_pages[j] : -1;
+                const int64_t j = j0 + u;
+                to[u] = -1;
+                if (u >= per || j < first || j >= end) continue;
+                while (off[i + 1] <= j) ++i;
+                to[u] = (int64_t)at[i].x * width + at[i].y + ((int32_t)j - off[i]);
+                page_no[u] = j < n_free ? free_pages[j] : -1;
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (to[u] >= 0) table[to[u]] = page_no[u];
         }
         __syncthreads();                           // read: the next round may overwrite it
     }
@@ -112,6 +129,9 @@ __global__ __launch_bounds__(kSlotThreads) void build_slots_kernel(const int32_t
     // Token of element e of a request: first + e, and from element `head` on `jump` more (a window's first tokens come before it).
     struct Request { int32_t row, first, head, jump; };
     __shared__ Request of[kSlotRequests];
+    const bool power = (page & (page - 1)) == 0;
+    const int shift = __builtin_ctz(page);
+    auto page_of = [&](uint32_t t) { return power ? t >> shift : t / (uint32_t)page; };
     int64_t base = 0;
     if (B == 0 && blockIdx.x == 0 && threadIdx.x == 0) seq_offsets[0] = 0;
     for (int64_t r0 = 0; r0 < B; r0 += kSlotRequests) {
@@ -125,23 +145,60 @@ __global__ __launch_bounds__(kSlotThreads) void build_slots_kernel(const int32_t
         if (blockIdx.x == 0)
             for (int i = threadIdx.x; i <= n; i += kSlotThreads) seq_offsets[r0 + i] = off[i];
         const int32_t first = off[0], end = off[n];
-        const int64_t c0 = first / kSlotChunk, turn = ((int64_t)blockIdx.x - c0 % gridDim.x + gridDim.x) % gridDim.x;
-        for (int64_t c = c0 + turn; c * kSlotChunk < end; c += gridDim.x) {
+        const int per = end - first <= kSlotThreads * (int64_t)gridDim.x ? 1 : 4, chunk = kSlotThreads * per;
+        for (int64_t c = first / chunk + blockIdx.x; c * chunk < end; c += gridDim.x) {
+            const int64_t j0 = c * chunk + per * (int64_t)threadIdx.x;
+            if (j0 + per <= first || j0 >= end) continue;
+            int i = find_request(off, n, (int32_t)max(j0, (int64_t)first));
+            Request r = of[i];
+            const int32_t e0 = (int32_t)j0 - off[i];
+            // four elements next to each other that are four tokens next to each other, in a row that has them all
+            if (per == 4 && j0 >= first && j0 + 4 <= off[i + 1] && (e0 >= r.head || e0 + 4 <= r.head) && r.row >= 0 && r.row < rows) {
+                const uint32_t t = (uint32_t)r.first + e0 + (e0 >= r.head ? r.jump : 0), p = page_of(t);
+                if (p < (uint32_t)width && page_of(t + 3) < (uint32_t)width) {
+                    const int32_t* const entries = table + ((int64_t)r.row * width + p);
+                    Int4 slot;
+                    if (page == 1) {
+                        slot = *(const Int4*)entries;
+                        slot = {max(slot.x, -1), max(slot.y, -1), max(slot.z, -1), max(slot.w, -1)};
+                    } else {
+                        int32_t to[4];
+                        const int32_t last = page_of(t + 3) - p;     // entries of the four, up to 4 (0: all on one page)
+                        const int32_t entry[4] = {entries[0], entries[min(1, last)], entries[min(2, last)], entries[last]};
+                        uint32_t at = t - p * page, of_page = 0;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int32_t x = of_page == 0 ? entry[0] : of_page == 1 ? entry[1] : of_page == 2 ? entry[2] : entry[3];
+                            to[u] = x >= 0 ? (int32_t)((uint32_t)x * page + at) : -1;
+                            if (++at == (uint32_t)page) { at = 0; ++of_page; }
+                        }
+                        slot = {to[0], to[1], to[2], to[3]};
+                    }
+                    *(Int4*)(slots + j0) = slot;
+                    const uint32_t at = (uint32_t)pos_first + t * (uint32_t)pos_stride;
+                    if (pos) *(Int4*)(pos + j0) = {(int32_t)at, (int32_t)(at + pos_stride), (int32_t)(at + 2 * (uint32_t)pos_stride), (int32_t)(at + 3 * (uint32_t)pos_stride)};
+                    continue;
+                }
+            }
+            int32_t entry[4];                                       // all loads before the first store: one round trip
+            uint32_t token[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t j = c * kSlotChunk + u * kSlotThreads + threadIdx.x;
-                if (j < first || j >= end) continue;
-                const int i = find_request(off, n, (int32_t)j);
-                const Request r = of[i];
+                const int64_t j = j0 + u;
+                if (u >= per || j < first || j >= end) continue;
+                while (off[i + 1] <= j) ++i;
+                r = of[i];
                 const int32_t e = (int32_t)j - off[i];
-                const uint32_t t = (uint32_t)r.first + e + (e >= r.head ? r.jump : 0), p = t / (uint32_t)page;
-                int32_t slot = -1;
-                if (r.row >= 0 && r.row < rows && p < (uint32_t)width) {
-                    const int32_t entry = table[(int64_t)r.row * width + p];
-                    if (entry >= 0) slot = (int32_t)((uint32_t)entry * page + (t - p * page));
-                }
-                slots[j] = slot;
-                if (pos) pos[j] = (int32_t)((uint32_t)pos_first + t * (uint32_t)pos_stride);
+                token[u] = (uint32_t)r.first + e + (e >= r.head ? r.jump : 0);
+                const uint32_t p = page_of(token[u]);
+                entry[u] = r.row >= 0 && r.row < rows && p < (uint32_t)width ? table[(int64_t)r.row * width + p] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t j = j0 + u;
+                if (u >= per || j < first || j >= end) continue;
+                slots[j] = entry[u] >= 0 ? (int32_t)((uint32_t)entry[u] * page + (token[u] - page_of(token[u]) * page)) : -1;
+                if (pos) pos[j] = (int32_t)((uint32_t)pos_first + token[u] * (uint32_t)pos_stride);
             }
         }
         __syncthreads();
@@ -149,15 +206,15 @@ __global__ __launch_bounds__(kSlotThreads) void build_slots_kernel(const int32_t
 }
 
 static unsigned slot_grid(int64_t elements) {
-    const int64_t chunks = (elements + kSlotChunk - 1) / kSlotChunk;
-    return (unsigned)(chunks < 1 ? 1 : chunks > 2048 ? 2048 : chunks);
+    const int64_t chunks = (elements + kSlotThreads - 1) / kSlotThreads;
+    return (unsigned)(chunks < 1 ? 1 : chunks > kSlotMost ? kSlotMost : chunks);
 }
 
 esp_status launch_extend_table(const int32_t* free_pages, int32_t n_free, const int32_t* req_row, const int32_t* old_lens, const int32_t* new_lens,
                                int32_t B, int32_t page, int32_t* table, int32_t rows, int32_t width, int32_t* taken, hipStream_t stream) {
     // (how many pages there are to place is not known here; a workgroup that finds none for it ends after the prefix sum)
     const int64_t most = (int64_t)B * width < n_free ? (int64_t)B * width : n_free;
-    hipLaunchKernelGGL(extend_table_kernel, dim3(slot_grid(most) < 256 ? slot_grid(most) : 256), dim3(kSlotThreads), 0, stream, free_pages, n_free, req_row,
+    hipLaunchKernelGGL(extend_table_kernel, dim3(slot_grid(most) < 512 ? slot_grid(most) : 512), dim3(kSlotThreads), 0, stream, free_pages, n_free, req_row,
                        old_lens, new_lens, B, page, table, rows, width, taken);
     return check_launch("extend_table_kernel");
 }
