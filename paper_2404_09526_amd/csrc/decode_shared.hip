@@ -7,8 +7,6 @@
 // memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
 // ranges side by side, and what bounds the one is left over by the other.  A second launch combines the partials of both kinds.
 #include <math.h>
-#include <stdlib.h>
-#include <stdio.h>
 
 #include "column_tile.h"
 #include "decode_merge.h"
@@ -23,10 +21,10 @@ constexpr int kSharedOwn = kSharedMost / kSharedWaves;              // keys of a
 constexpr int kSharedLds = 2 * kSharedHalf + kSharedMost * 4;
 // tiles that wavefronts have for themselves lie before the lists; the blocks of the combination, which are larger, may lie on them: it comes last
 static_assert(kSharedWaves * kSharedTile <= 2 * kSharedHalf && kSharedWaves * kColWaveBytes <= kSharedLds, "the wavefronts' tiles and blocks fit");
-// The offset that probabilities are taken against is moved (and the accumulators with it) only where a score lies this far above it, in log2:
-// moved with every new maximum, as the plain decode's, it moves in half of the tiles for some column of the 32.  Probabilities are up to
-// 2^8 then, which changes nothing for their bf16 or the fp32 sums.
-constexpr float kSharedSlack = 8.f;
+// The offset that a wide workgroup takes probabilities against is moved (and the accumulators with it) only where those of a tile sum up to more than
+// this: moved with every new maximum, as the plain decode's, it moves in half of the tiles for some column of the 32.  Larger
+// probabilities change nothing for their bf16 or the fp32 sums.
+constexpr float kSharedSum = 4096.f;
 
 struct SharedParts { float* acc; float* ml; int32_t range; };
 // The work of the first launch: `prefix` workgroups on the prefix (units (range, KV head), `blocks` column blocks each) and `own` on the requests' own
@@ -172,7 +170,6 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
     const RequestRange& at = part.at;
     const int32_t t0 = at.t0, b0 = part.b0, seg = part.seg, n_all = part.n_all, kvh = part.kvh, G = a.Hq / a.Hkv;
     if (n_all <= (int32_t)cb * (32 * COLS)) return;
-    const bool once = n_all <= 32 * COLS;                           // the only workgroup on these rows
     const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = n_all - rho0;   // (columns of this wavefront, up to 32; none: it only moves tiles)
 
     int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf);
@@ -208,6 +205,11 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
         // A wavefront's rows of a tile are the same for K and V: slots are looked up a group ahead, and a row's place is kept from K's group to V's.
         uint32_t slot[MOVES];
         uint64_t place[MOVES];
+        // (Up to four column tiles are all that there are, and the rows pass once.  Of eight there may be more workgroups on the same rows.)
+        auto fetch_row = [](uint32_t to, const char* from) {
+            if constexpr (COLS < 8) load_to_lds_b128_at_nt(to, from);
+            else load_to_lds_b128_at(to, from);
+        };
         auto look_up = [&](int i) {
 #pragma unroll
             for (int x = 0; x < MOVES; ++x) slot[x] = (uint32_t)list[min(i * STEP + team * 32 + col_row(ct + COLS * x, lane), seg - 1)];
@@ -218,16 +220,14 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
                 const int n = ct + COLS * x;
                 place[x] = (uint64_t)slot[x] * row_bytes;
                 const uint32_t to = __builtin_amdgcn_readfirstlane(k_tile(i) + 1024 * n);
-                if (once) load_to_lds_b128_at_nt(to, kbase + (place[x] + col_k_within(n, lane)));
-                else load_to_lds_b128_at(to, kbase + (place[x] + col_k_within(n, lane)));
+                fetch_row(to, kbase + (place[x] + col_k_within(n, lane)));
             }
         };
         auto fetch_v = [&](int i) {
 #pragma unroll
             for (int x = 0; x < MOVES; ++x) {
                 const uint32_t to = __builtin_amdgcn_readfirstlane(v_tile(i) + 1024 * (ct + COLS * x));
-                if (once) load_to_lds_b128_at_nt(to, vbase + (place[x] + col_v_within(lane)));
-                else load_to_lds_b128_at(to, vbase + (place[x] + col_v_within(lane)));
+                fetch_row(to, vbase + (place[x] + col_v_within(lane)));
             }
         };
         auto fetch_group = [&](int j) {
@@ -297,11 +297,27 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
                     for (int r = 0; r < 16; ++r)
                         if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
                 }
-                float top = sc[0];
+                // Probabilities against the offset in use, without a look at the scores first; their sums tell whether it has to move.
+                float sum, sum_r;
+                auto weigh = [&] {
+                    const float sub = cols.m == -INFINITY ? 0.f : cols.m;
+                    sum = sum_r = 0.f;
 #pragma unroll
-                for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
-                top = half_swap_max(top) * scale_log2;
-                if (__builtin_amdgcn_ballot_w64(top > cols.m + kSharedSlack) != 0) {
+                    for (int c = 0; c < 8; ++c) {
+                        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c], scale_log2, -sub));
+                        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c + 1], scale_log2, -sub));
+                        sum += p0 + p1;
+                        const uint32_t pk = pack_bf16(p0, p1);
+                        sum_r = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum_r, false);
+                        pf[c >> 2].u[c & 3] = pk;
+                    }
+                };
+                weigh();
+                if (__builtin_amdgcn_ballot_w64(sum > kSharedSum || cols.m == -INFINITY) != 0) {
+                    float top = sc[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+                    top = half_swap_max(top) * scale_log2;
                     // (a column that has seen nothing but -inf and NaN stays as it is: exp2(-inf - -inf) must not leak into sums that are zero)
                     const float to = fmaxf(cols.m, top), alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(cols.m - to);
                     cols.m = to;
@@ -310,17 +326,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
                     for (int db = 0; db < 4; ++db)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) cols.oacc[db][r] *= alpha;
-                }
-                const float sub = cols.m == -INFINITY ? 0.f : cols.m;
-                float sum = 0.f, sum_r = 0.f;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c], scale_log2, -sub));
-                    const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c + 1], scale_log2, -sub));
-                    sum += p0 + p1;
-                    const uint32_t pk = pack_bf16(p0, p1);
-                    sum_r = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum_r, false);
-                    pf[c >> 2].u[c & 3] = pk;
+                    weigh();
                 }
                 cols.l += sum; cols.l_r += sum_r;
             }
@@ -502,58 +508,49 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
 
 // The ranges of both kinds, and the workgroups that they are.
 struct SharedPlan {
-    int32_t cols, range, own_range;                                 // column tiles of a workgroup on the largest group's prefix; keys of a range
+    int32_t range, own_range;                                       // keys of a range
     size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
 };
-// One workgroup a CU, whichever kind.  A workgroup on the prefix takes a start, its steps, and an end whose partial is written and read at the memory's
-// rate; one on own rows a start and, when the memory is not what it waits for, 2.5 us for each 32 keys of its longest wavefront.  Own ranges first: the
-// least of what all of them take and a third of the longest; then of the prefix' possible ranges the one whose rounds, alone, or whose share of the chip's time
-// beside the own ranges, is the least.
+// One workgroup a CU, whichever kind.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least: a workgroup
+// on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and a third
+// of the longest at the end, or, where they are only a few rounds of the chip, whole rounds; the longest alone; all rows at the memory's rate.  What is not
+// known is how the groups differ: several are taken to be as large as their average.  Measured on 92 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of
+// 0 .. 110000 tokens, thirteen head layouts) with 66 choices each, the estimates' choice was 5.6 % from the best on average; with the largest group in
+// place of the average 7.3 %, with one fixed choice for all (512 and 128) 21 %.
 static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 2.5;
+    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 3.3, kTail = 0.33, kFewRounds = 2.5, kWholeRound = 1.2, kPartial = 0.0105, kBytesPerUs = 6.4e6;
     struct Times { double start, step; };
-    constexpr Times kTimes[4] = {{7, 5.3}, {8, 2.9}, {9, 1.3}, {9, 1.15}};   // us, of a workgroup with 1, 2, 4, 8 column tiles
+    constexpr Times kTimes[4] = {{7, 4.5}, {8, 2.7}, {9, 1.25}, {10, 1.15}};   // of a workgroup with 1, 2, 4, 8 column tiles
+    constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
+    static_assert(kRanges[10] == kSharedMost && kOwnRanges[5] == kSharedOwn, "their slots lie in LDS");
     SharedPlan p = {};
-    const int64_t G = Hq / Hkv, rows = max_group * G, chunks = (G + 31) / 32;
-    p.cols = shared_cols(rows);
-    const int kind = __builtin_ctz(p.cols);
-    p.blocks = (rows + 32 * p.cols - 1) / (32 * p.cols);
-
-    double own_us = 0;
-    auto own_wgs = [&](int64_t range) { return ((total_tokens / range + B) * Hkv * chunks + kSharedWaves - 1) / kSharedWaves; };
-    p.own_range = 32;
-    if (total_tokens > 0) {
-        const double tiles = (double)total_tokens / 32 * Hkv * chunks / kSharedWaves;
-        for (int32_t range = 64; range <= kSharedOwn; range += range < 256 ? 64 : 128) {
-            const double us = ((double)own_wgs(range) * kOwnStart + tiles * kOwnTile) / kCus + 0.35 * (kOwnStart + kOwnTile * range / 32);
-            if (range == 64 || us < own_us) { own_us = us; p.own_range = range; }
+    const int64_t G = Hq / Hkv, chunks = (G + 31) / 32, mean = n_groups > 1 ? (B + n_groups / 2) / n_groups : max_group, rows = (mean > 1 ? mean : 1) * G;
+    const int cols = shared_cols(rows), kind = __builtin_ctz(cols);
+    const int64_t step = 32 * (kSharedWaves / cols), wide = Hkv * ((rows + 32 * cols - 1) / (32 * cols));
+    const double own_tiles = (double)total_tokens / 32 * Hkv * chunks / kSharedWaves;
+    const double memory = ((double)prefix_total + total_tokens) * Hkv * (4 * kHeadDim) / kBytesPerUs;
+    auto own_wgs = [&](int32_t range) { return total_tokens == 0 ? 0 : (((int64_t)total_tokens / range + B) * Hkv * chunks + kSharedWaves - 1) / kSharedWaves; };
+    double best_us = HUGE_VAL;
+    for (const int32_t range : kRanges) {
+        const double one = kTimes[kind].start + kTimes[kind].step * (double)((range + step - 1) / step);
+        const double wgs = ((double)(prefix_total / range + 1) + 0.5 * (n_groups - 1)) * wide, prefix_us = wgs * one;
+        for (const int32_t own_range : kOwnRanges) {
+            const double own = (double)own_wgs(own_range), longest = total_tokens == 0 ? one : fmax(one, kOwnStart + kOwnTile * own_range / 32);
+            const double sum = prefix_us + own * kOwnStart + own_tiles * kOwnTile, n = wgs + own;
+            double us = fmax(fmax(sum / kCus + kTail * longest, longest), memory);
+            if (n <= kFewRounds * kCus) us = fmax(us, kWholeRound * ceil(n / kCus) * sum / n);
+            us += wgs * cols * kPartial;
+            if (us < best_us) { best_us = us; p.range = range; p.own_range = own_range; }
+            if (total_tokens == 0) break;
         }
-        p.own = own_wgs(p.own_range);
+        if (range >= prefix_total) break;
     }
-    p.own_slots = (size_t)(total_tokens / p.own_range + B);         // (of requests of any lengths)
-
-    const int64_t step = 32 * (kSharedWaves / p.cols), steps = ((int64_t)prefix_total + step - 1) / step, wide = Hkv * p.blocks;
-    const double partial_us = p.cols * 0.009;
-    double best_us = 0;
-    int64_t best = 1;
-    auto consider = [&](int64_t ranges) {
-        int64_t take = ranges < 1 ? steps : (steps + ranges - 1) / ranges;
-        if (take > kSharedMost / step) take = kSharedMost / step;
-        if (take < 1) take = 1;
-        const double wgs = (double)((steps + take - 1) / take + n_groups - 1) * wide, one = kTimes[kind].start + kTimes[kind].step * take;
-        const double alone = ceil(wgs / kCus) * one, beside = (wgs * one) / kCus + own_us + 0.35 * one;
-        const double us = (own_us < 0.5 * one ? alone + own_us : beside) + wgs * partial_us;
-        if (best_us == 0 || us < best_us) { best_us = us; best = take; }
-    };
-    for (int64_t ranges = 1; ranges <= steps && ranges * wide <= 8192; ranges += 1 + ranges / 6) consider(ranges);
-    for (int64_t rounds = 1; rounds <= 8; ++rounds) consider(rounds * (int64_t)kCus / wide - (n_groups - 1));
-    if (getenv("XR")) best = atoi(getenv("XR")) / step; if (best < 1) best = 1; if (best > kSharedMost / step) best = kSharedMost / step;
-    if (getenv("XO") && total_tokens > 0) { p.own_range = atoi(getenv("XO")); p.own = own_wgs(p.own_range); p.own_slots = (size_t)(total_tokens / p.own_range + B); }
-    p.range = (int32_t)(best * step);
+    p.blocks = (max_group * G + 255) / 256;                         // (fewer than eight column tiles are one block)
     p.slots = (size_t)(prefix_total / p.range) + n_groups;
     p.units = (int64_t)p.slots * Hkv;
-    if (getenv("XV")) printf("cols %d range %d own %d wgs %ld + %ld est %.1f (own %.1f)\n", p.cols, p.range, p.own_range, (long)(p.units * p.blocks), (long)p.own, best_us, own_us);
+    p.own = own_wgs(p.own_range);
+    p.own_slots = (size_t)(total_tokens / p.own_range + B);         // (of requests of any lengths)
     return p;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
