@@ -75,9 +75,10 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
 
 // Ranges counted from each list's first token on (lists: offsets[b] .. offsets[b + 1]), all whole ones first, then what is left of each list: where
 // range i is, as request_range (esp_common.h) finds it, but 64 N lists at a time, whose offsets are one round trip for both kinds where that is all.
+// members: offsets of something else by list, whose bounds for the list that is found go to m0 and m1 (asked for together with its own).
 template <int N>
-__device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int lane) {
-    int32_t s0[N], s1[N];
+__device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int lane, const int32_t* members, int32_t& m0, int32_t& m1) {
+    int32_t s0[N], s1[N], of0[N], of1[N];
 #pragma unroll 1
     for (int rest = 0; rest < 2; ++rest) {
 #pragma unroll 1
@@ -87,6 +88,7 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
                 for (int u = 0; u < N; ++u) {
                     const int b = min(base + 64 * u + lane, B - 1);
                     s0[u] = offsets[b]; s1[u] = offsets[b + 1];
+                    if (members) { of0[u] = members[b]; of1[u] = members[b + 1]; }
                 }
             }
 #pragma unroll
@@ -106,6 +108,7 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
                     const int32_t start = __builtin_amdgcn_readlane(s0[u], l), end = __builtin_amdgcn_readlane(s1[u], l);
                     const int32_t part = rest ? __builtin_amdgcn_readlane(whole, l) : i - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
                     const int32_t t0 = start + part * range;
+                    if (members) { m0 = __builtin_amdgcn_readlane(of0[u], l); m1 = __builtin_amdgcn_readlane(of1[u], l); }
                     return {base + 64 * u + l, t0, t0 + min(range, end - t0), start / range + part};
                 }
                 i -= __builtin_amdgcn_readlane(upto, 63);
@@ -122,7 +125,8 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
     const int G = a.Hq / a.Hkv, chunks = (G + 31) / 32;
     const uint32_t unit = (uint32_t)index * kSharedWaves + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
     const int kvh = rest / (uint32_t)chunks, g0 = (rest - kvh * chunks) * 32, ng = min(32, G - g0), h0 = kvh * G + g0;
-    const RequestRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, lane);
+    int32_t none;
+    const RequestRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, lane, nullptr, none, none);
     const int32_t seg = min(at.t1, a.total_tokens) - at.t0;         // (never past the slot list)
     if (seg <= 0) return;
     int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf) + wave * kSharedOwn;
@@ -419,9 +423,10 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(Sh
     if (unit >= (uint32_t)work.units) return;
     PrefixPart part;
     part.kvh = unit % (uint32_t)a.Hkv;
-    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane);
-    part.b0 = a.group_offsets[part.at.b];
-    part.n_all = min(min(a.group_offsets[part.at.b + 1], a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
+    int32_t b1 = 0;
+    part.b0 = 0;
+    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane, a.group_offsets, part.b0, b1);
+    part.n_all = min(min(b1, a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
     part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
     if (part.seg <= 0 || part.n_all <= 0) return;
     switch (shared_cols(part.n_all)) {
@@ -460,13 +465,21 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
             sum.template add<false>(m, l, v);
         }
     };
-    if (a.prefix_total > 0) {
-        const RequestAt in = request_of(b, a.group_offsets, a.n_groups, threadIdx.x & 63);
-        const int32_t b0 = a.group_offsets[in.b], p0 = a.prefix_offsets[in.b], p1 = min(a.prefix_offsets[in.b + 1], a.prefix_total);
-        if (b >= b0 && b < in.end && b - b0 < a.max_group && p1 > p0) {
+    // the pair's group, and where its prefix lies: 64 groups at a time, their bounds asked for together
+    const int l64 = threadIdx.x & 63;
+#pragma unroll 1
+    for (int base = 0; base < a.n_groups; base += 64) {
+        const int of = min(base + l64, a.n_groups - 1);
+        const int32_t g0 = a.group_offsets[of], g1 = a.group_offsets[of + 1], p0 = a.prefix_offsets[of], p1 = min(a.prefix_offsets[of + 1], a.prefix_total);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(g0 <= b && b < g1);
+        if (!hit) continue;
+        const int l = __builtin_ctzll(hit);
+        const int32_t b0 = __builtin_amdgcn_readlane(g0, l), from = __builtin_amdgcn_readlane(p0, l), to = __builtin_amdgcn_readlane(p1, l);
+        if (b - b0 < a.max_group && to > from) {
             const int64_t rows = (int64_t)a.max_group * a.Hq;
-            add(parts.acc, parts.ml, (int64_t)(p0 / parts.range + in.b) * rows + (int64_t)(b - b0) * a.Hq + h, rows, (p1 - p0 - 1) / parts.range + 1);
+            add(parts.acc, parts.ml, (int64_t)(from / parts.range + base + l) * rows + (int64_t)(b - b0) * a.Hq + h, rows, (to - from - 1) / parts.range + 1);
         }
+        break;
     }
     if (s1 > s0) add(mine.acc, mine.ml, ((int64_t)(s0 / mine.range) + b) * a.Hq + h, a.Hq, own_partials(s0, s1, mine.range, mine.parts));
 
@@ -534,7 +547,7 @@ static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total,
     double best_us = HUGE_VAL;
     for (const int32_t range : kRanges) {
         const double one = kTimes[kind].start + kTimes[kind].step * (double)((range + step - 1) / step);
-        const double wgs = ((double)(prefix_total / range + 1) + 0.5 * (n_groups - 1)) * wide, prefix_us = wgs * one;
+        const double wgs = (ceil((double)prefix_total / range) + 0.5 * (n_groups - 1)) * wide, prefix_us = wgs * one;
         for (const int32_t own_range : kOwnRanges) {
             const double own = (double)own_wgs(own_range), longest = total_tokens == 0 ? one : fmax(one, kOwnStart + kOwnTile * own_range / 32);
             const double sum = prefix_us + own * kOwnStart + own_tiles * kOwnTile, n = wgs + own;
@@ -583,7 +596,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair
 #define ESP_COMBINE_LAUNCH(GROUPS)                                                                                                          \
     hipLaunchKernelGGL((shared_combine_kernel<GROUPS>), row_grid(((int64_t)pairs + 8 / GROUPS - 1) / (8 / GROUPS)), dim3(256), 0, stream, a, pairs, parts, mine)
-    if (most <= 32) ESP_COMBINE_LAUNCH(2);
+    if (most <= 64) ESP_COMBINE_LAUNCH(2);
     else ESP_COMBINE_LAUNCH(8);
 #undef ESP_COMBINE_LAUNCH
     return check_launch("shared_combine_kernel");
