@@ -174,6 +174,7 @@ int32_t set_decode_plan(int32_t plan) {
     t_forced_decode = plan;
     return before;
 }
+int32_t forced_decode_plan() { return t_forced_decode; }
 int32_t query_decode_plan(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv) {
     return decode_whole(B, total_tokens, max_len, Hq, Hkv) ? 2 : 1;
 }

@@ -437,6 +437,89 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(Sh
     }
 }
 
+// Few short requests, in one launch: a workgroup has one request and KV head (a chunk of its query heads) and walks the prefix and the
+// request's own rows as one list (as decode_whole.hip does with one); the prefix is read by each, from the caches, and no combination follows.
+__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(SharedArgs a, float scale_log2) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedWaves * kColWaveBytes];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int qi = lane & 31, hi = lane >> 5;
+    const int b = blockIdx.x, kvh = blockIdx.y;
+    const int32_t s0 = a.seq_offsets[b], s1 = min(a.seq_offsets[b + 1], a.total_tokens);   // (never past the slot list)
+    int32_t p0 = 0, P = 0;
+#pragma unroll 1
+    for (int base = 0; base < a.n_groups; base += 64) {
+        const int of = min(base + lane, a.n_groups - 1);
+        const int32_t g0 = a.group_offsets[of], g1 = a.group_offsets[of + 1], from = a.prefix_offsets[of], to = min(a.prefix_offsets[of + 1], a.prefix_total);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(g0 <= b && b < g1);
+        if (!hit) continue;
+        const int l = __builtin_ctzll(hit);
+        p0 = __builtin_amdgcn_readlane(from, l);
+        if (b - __builtin_amdgcn_readlane(g0, l) < a.max_group) P = max(__builtin_amdgcn_readlane(to, l) - p0, 0);
+        break;
+    }
+    const uint32_t n = (uint32_t)P + max(s1 - s0, 0);               // (without a sign: tiles that are looked ahead to may start past 2^31)
+    const int32_t *const prefix = a.prefix_slots + p0, *const own = a.slot_idx + s0;
+    auto tile_slots = [&](uint32_t i) {                             // lane: of tile row lane % 32 (rows past the end: the last)
+        const uint32_t t = min(32 * i + qi, n - 1);
+        return t < (uint32_t)P ? prefix[t] : own[t - P];
+    };
+    int32_t slots = 0, slots_next = 0;
+    if (32 * wave < n) { slots = tile_slots(wave); slots_next = tile_slots(wave + kSharedWaves); }
+    const int G = a.Hq / a.Hkv, g0 = blockIdx.z * 32, ng = min(32, G - g0);
+    const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
+    const char* kbase = a.k_pool + (uint32_t)kvh * (kHeadDim * 2);
+    const char* vbase = a.v_pool + (uint32_t)kvh * (kHeadDim * 2);
+    const uint32_t lds_k = (uint32_t)(uintptr_t)(ESP_LDS unsigned char*)smem + wave * kColWaveBytes;
+    const int64_t pair = (int64_t)b * a.Hq + kvh * G + g0 + min(qi, ng - 1);   // of this column (past the chunk: the last one's, nothing written)
+    bf16x8 qf[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) qf[t] = *(const bf16x8*)((const uint16_t*)a.q + pair * kHeadDim + 16 * t + 8 * hi);
+    asm volatile("" : "+v"(slots), "+v"(slots_next) : "v"(qf[0]), "v"(qf[1]), "v"(qf[2]), "v"(qf[3]), "v"(qf[4]), "v"(qf[5]), "v"(qf[6]), "v"(qf[7]));   // here before the transfers, whose waits count
+    Columns cols;
+    cols.place(lds_k, lane);
+    cols.clear();
+    auto fetch = [&](uint32_t to, const char* base, int32_t of, bool is_k) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            load_to_lds_b128_at(to + 1024 * x, base + ((uint64_t)(uint32_t)__shfl(of, col_row(x, lane)) * row_bytes + (is_k ? col_k_within(x, lane) : col_v_within(lane))));
+    };
+    if (32 * wave < n) { fetch(lds_k, kbase, slots, true); fetch(lds_k + kColKBytes, vbase, slots, false); }
+    for (uint32_t i = wave; 32 * i < n; i += kSharedWaves) {
+        const int here = min(32u, n - 32 * i);
+        const bool next = 32 * (i + kSharedWaves) < n;
+        wait_vm<8>();                                               // K has landed; V may be on its way
+        floatx16 sc = cols.scores(qf);
+        if (next) {
+            asm volatile("" :: "v"(sc));                            // K has been read
+            fetch(lds_k, kbase, slots_next, true);
+        }
+        if (here < 32) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
+        }
+        Columns::PFrag pf[2];
+        cols.weigh(sc, scale_log2, pf);
+        if (next) wait_vm<8>(); else wait_vm<0>();
+        cols.accumulate(pf);
+        if (next) {
+            fetch(lds_k + kColKBytes, vbase, slots_next, false);
+            slots_next = tile_slots(i + 2 * kSharedWaves);
+        }
+    }
+    constexpr int N = 64 / kSharedWaves;
+    float out[N], mx, lsum;
+    cols.combine<kSharedWaves>(smem, wave, lane, out, mx, lsum);
+    if (qi >= ng) return;
+    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;              // no token: 0; a NaN shows
+    const int at = Columns::first_element<kSharedWaves>(wave, lane);
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+        ((U32x2*)a.O)[(pair * kHeadDim + at + 2 * e) / 4] = U32x2{pack_bf16(out[e] * inv, out[e + 1] * inv), pack_bf16(out[e + 2] * inv, out[e + 3] * inv)};
+    if (wave == 0 && hi == 0) a.LSE[pair] = lsum == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(lsum)) * kLn2;
+}
+
 // Combination, as the plain decode's (decode.hip): groups of 32 lanes take a pair's partials in turn, four at a time, first those of the
 // prefix, then its own.
 template <int GROUPS>
@@ -524,6 +607,8 @@ struct SharedPlan {
     int32_t range, own_range;                                       // keys of a range
     size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
+    double us;                                                      // the estimate
+    int kind;                                                       // column tiles of a workgroup for an average group, 2^kind
 };
 // One workgroup a CU, whichever kind.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least: a workgroup
 // on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and a third
@@ -559,6 +644,8 @@ static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total,
         }
         if (range >= prefix_total) break;
     }
+    p.us = best_us;
+    p.kind = kind;
     p.blocks = (max_group * G + 255) / 256;                         // (fewer than eight column tiles are one block)
     p.slots = (size_t)(prefix_total / p.range) + n_groups;
     p.units = (int64_t)p.slots * Hkv;
@@ -575,13 +662,35 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
     return partials_bytes(p.slots, (int64_t)max_group * Hq) + partials_bytes(p.own_slots, Hq);
 }
 
+// Which calls run in one launch: those with no more workgroups than CUs whose estimate is the less.  In one launch: a start and an end, then the longest
+// list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 290
+// calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
+// 20 behind 300, 4 / 4 heads, 12.1 -> 8.4, of 300 behind 1000 13.2 -> 16.1*; 16 of 300 behind 30, 32 / 8, 17.3 -> 10.5, 16 of 20 behind 1000 16.0 -> 14.5, behind
+// 2000 17.3 -> 22.0*; 32 of 300 behind 300, 32 / 1, 21.2 -> 14.0.  To the better form the choice loses 0.3 % on average, 18 % at most.
+static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
+    const int32_t forced = forced_decode_plan();
+    if (forced != 0) return forced == 2;
+    const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
+    if (a.B * (int64_t)a.Hkv * chunks > 256) return false;
+    const double bytes = ((double)a.B * a.max_prefix + a.total_tokens) * a.Hkv * chunks * (4 * kHeadDim);
+    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 3.1 + 0.8 * p.us + 1.8 * p.kind;
+    return whole < 0.95 * ranges;
+}
+
 esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_t stream) {
     if (a.prefix_total == 0 || a.max_group == 0)
         return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
                              workspace, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream);
     if ((int64_t)a.B * a.Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode (shared): too many rows for one launch");
-    const int32_t pairs = a.B * a.Hq;
     const SharedPlan p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
+    if (shared_whole(a, p)) {
+        const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
+        if (a.B > (int32_t)(UINT32_MAX / (kSharedWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
+            return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many requests or heads for one launch of a workgroup each");
+        hipLaunchKernelGGL(shared_whole_kernel, dim3(a.B, a.Hkv, (unsigned)chunks), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e);
+        return check_launch("shared_whole_kernel");
+    }
+    const int32_t pairs = a.B * a.Hq;
     const int64_t prefix = (p.units + 7) / 8 * 8 * p.blocks, own = (p.own + 7) / 8 * 8;
     if (prefix + own > (int64_t)(UINT32_MAX / (kSharedWaves * 64)) || p.units > INT32_MAX / 2)
         return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");

@@ -187,6 +187,7 @@ esp_status launch_decode_whole(const void* q, const void* k_pool, const void* v_
 // whether decode calls of this thread work in ranges (1), in one launch (2), or by estimate (0); returns the previous value; and what a
 // call of these sizes would do
 int32_t set_decode_plan(int32_t plan);
+int32_t forced_decode_plan();     // what was set
 int32_t query_decode_plan(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv);
 
 int32_t set_prefill_sync_ticks(int32_t ticks);   // returns the previous value; negative restores the built-in default

@@ -315,8 +315,16 @@ SHARED = [
 ]
 
 
+@pytest.fixture(params=[0, 1, 2], ids=["by-estimate", "ranges", "one-launch"])
+def form(request, cuda):
+    """The calls in ranges and a combination, in one launch, and as the estimates say: what the tests claim, they claim of all."""
+    before = esp.esp_debug_set_decode_plan(request.param)
+    yield request.param
+    assert esp.esp_debug_set_decode_plan(before) == request.param
+
+
 @pytest.mark.parametrize("name,groups,prefixes,lens,Hq,Hkv", SHARED, ids=[s[0] for s in SHARED])
-def test_decode_behind_shared_prefixes(cuda, name, groups, prefixes, lens, Hq, Hkv):
+def test_decode_behind_shared_prefixes(cuda, form, name, groups, prefixes, lens, Hq, Hkv):
     call, both = shared_inputs(cuda, groups, prefixes, lens, Hq, Hkv, 11)
     Or, Lr = shared_reference(call, both, cuda)
     O = torch.full(call["q"].shape, 7.0, dtype=torch.bfloat16, device=cuda)
@@ -328,7 +336,7 @@ def test_decode_behind_shared_prefixes(cuda, name, groups, prefixes, lens, Hq, H
     assert torch.equal(O, O2) and torch.equal(LSE, L2)
 
 
-def test_shared_bounds_larger_than_what_is_there(cuda):
+def test_shared_bounds_larger_than_what_is_there(cuda, form):
     call, both = shared_inputs(cuda, [3, 2], [200, 90], [5, 0, 7, 9, 1], 8, 2, 5)
     Or, Lr = shared_reference(call, both, cuda)
     call.update(max_prefix=290, max_group=5, max_len=22)
@@ -336,7 +344,7 @@ def test_shared_bounds_larger_than_what_is_there(cuda):
     check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), "bounds")
 
 
-def test_shared_without_groups_is_plain_decode(cuda):
+def test_shared_without_groups_is_plain_decode(cuda, form):
     call, both = shared_inputs(cuda, [3], [0], [50, 0, 7], 8, 2, 6)
     Or, Lr = shared_reference(call, both, cuda)
     none, zero = torch.empty(0, dtype=torch.int32, device=cuda), i32([0], cuda)
@@ -345,7 +353,7 @@ def test_shared_without_groups_is_plain_decode(cuda):
     check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), "no groups")
 
 
-def test_shared_rows_past_4_gb_of_the_pool(cuda):
+def test_shared_rows_past_4_gb_of_the_pool(cuda, form):
     call, both = shared_inputs(cuda, [40, 2], [700, 130], [9] * 42, 16, 8, 9, num_slots=(1 << 22) + 5)
     Or, Lr = shared_reference(call, both, cuda)
     O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=shared_workspace(call, cuda))
@@ -353,7 +361,7 @@ def test_shared_rows_past_4_gb_of_the_pool(cuda):
 
 
 @pytest.mark.parametrize("columns", [4, 60, 120, 250])
-def test_shared_nan_and_infinite_keys_show_where_they_are_seen(cuda, columns):
+def test_shared_nan_and_infinite_keys_show_where_they_are_seen(cuda, form, columns):
     n = columns // 2
     call, _ = shared_inputs(cuda, [n, n], [300, 310], [3] * (2 * n), 2, 2, 13)
     where = call["prefix_slots"][310].long()                           # a key of the second group's prefix
@@ -373,7 +381,7 @@ def test_shared_nan_and_infinite_keys_show_where_they_are_seen(cuda, columns):
     assert torch.equal(O[seen], call["v_pool"][last].expand_as(O)[seen])
 
 
-def test_shared_scores_far_apart(cuda):
+def test_shared_scores_far_apart(cuda, form):
     """Prefix and own tokens whose scores differ by hundreds, either way: the smaller side weighs nothing and leaves no NaN."""
     for at in ("prefix_slots", "slot_idx"):
         call, both = shared_inputs(cuda, [40], [200], [33] * 40, 4, 2, 21)
