@@ -402,8 +402,8 @@ size_t esp_decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t pr
  *   k_out, v_out bf16 [T,Hkv,D] dense, or NULL: the rows for a prefill call.  May be k and v themselves where those are dense.
  *   slot_idx int32 [T], k_pool, v_pool [num_slots,Hkv,D]: all NULL, or rows with a
  *     slot in [0, num_slots) are written there (slots must be distinct).
- * Outputs overlap their input only where they are it, and nothing else (a different overlap of q_out with
- * q, k_out with k or v_out with v is refused, ESP_ERR_INVALID_ARG).  Bulk pointers and
+ * Outputs overlap their input only where they are it, and nothing else (q_out next to q, or over q with other strides, is
+ * told apart and refused where rows meet: ESP_ERR_INVALID_ARG; so are k_out with k and v_out with v).  Bulk pointers and
  * weights lie on 16 bytes (ESP_ERR_INVALID_ARG).
  */
 esp_status esp_qk_norm_rope_append(

@@ -105,13 +105,12 @@ struct Columns {
     // goes to row rho of the wavefront's block (64 lanes x 4 bytes a row), maximum and sum to two more.  Wavefront j combines
     // the registers from 64 / WAVES * j on of all of them into out, with the column's maximum mx and sum lsum.  out[e] is
     // element first_element() + 2 e + e' of the column for e = 0, 4, ... and e' = 0 .. 3.
-    // STRIDE: the blocks of wavefronts that share their columns lie so many apart (smem: the first of them, wave: which of them this is).
-    template <int WAVES, int STRIDE = 1>
+    template <int WAVES>
     __device__ __forceinline__ void combine(unsigned char* smem, int wave, int lane, float (&out)[64 / WAVES], float& mx, float& lsum) const {
         constexpr int N = 64 / WAVES;
         const float l_tot = half_swap_sum(l), lr_tot = half_swap_sum(l_r);
         const float fix = lr_tot > 0.f ? l_tot / lr_tot : 0.f;
-        float* mine = (float*)(smem + wave * (STRIDE * kColWaveBytes));
+        float* mine = (float*)(smem + wave * kColWaveBytes);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -123,7 +122,7 @@ struct Columns {
         mx = -INFINITY;
 #pragma unroll
         for (int u = 0; u < WAVES; ++u) {
-            mw[u] = ((const float*)(smem + u * (STRIDE * kColWaveBytes)))[64 * 64 + lane];
+            mw[u] = ((const float*)(smem + u * kColWaveBytes))[64 * 64 + lane];
             mx = fmaxf(mx, mw[u]);
         }
         lsum = 0.f;
@@ -131,7 +130,7 @@ struct Columns {
         for (int e = 0; e < N; ++e) out[e] = 0.f;
 #pragma unroll
         for (int u = 0; u < WAVES; ++u) {
-            const float* blk = (const float*)(smem + u * (STRIDE * kColWaveBytes));
+            const float* blk = (const float*)(smem + u * kColWaveBytes);
             const float lu = blk[65 * 64 + lane];
             // a wavefront that saw no key (sum 0) has nothing to add; a NaN sum shows in lu * c
             const float c = lu > 0.f ? __builtin_amdgcn_exp2f(mw[u] - mx) : 0.f;

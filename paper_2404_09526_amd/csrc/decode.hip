@@ -86,7 +86,7 @@ static bool decode_burst_layout(int32_t Hq, int32_t Hkv) {
 // rounds of 256, 479 of 640 are one of 512.
 // `room`: ranges that the workspace holds (as far as the built-in block would, so that both calls agree); `kept`: ranges that
 // every workspace holds which is not refused (those of a simpler rule, by which workspaces are also measured).
-int32_t decode_range(int32_t total_tokens, int64_t step, int64_t least, int64_t rows, int64_t kept, int64_t room) {
+static int32_t decode_range(int32_t total_tokens, int64_t step, int64_t least, int64_t rows, int64_t kept, int64_t room) {
     constexpr int64_t kResident = 512;
     constexpr double kStart = 6, kStep = 4.8;                     // microseconds
     const double lag = rows > 1 ? 0.08 : 0;
@@ -454,8 +454,9 @@ __global__ __launch_bounds__(256) void decode_combine_kernel(const int32_t* __re
     const int32_t s0 = seq_offsets[b], s1 = seq_offsets[b + 1];
     Weighted<4> sum;
     if (s1 > s0) {
-        const int64_t first = s0 / range + b;                       // the slots of consecutive ranges
-        const int n = own_partials(s0, s1, range, parts);
+        const int w_lo = s0 / range;
+        const int64_t first = w_lo + b;                             // the slots of consecutive ranges
+        const int whole = (s1 - s0 - 1) / range + 1, n = parts == 0 ? (s1 - 1) / range - w_lo + 1 : parts > 0 ? min(parts, whole) : whole;
         for (int i = g; i < n; i += GROUPS * U) {
             float m[U], l[U];
             float v[U][4];
@@ -546,15 +547,20 @@ esp_status launch_decode_static(const void* q, const void* k_pool, const void* v
                          (size_t)ESP_DECODE_STATIC_SCRATCH_BYTES, stream);
 }
 
-esp_status launch_decode_partials(const void* q, const void* k_pool, const void* v_pool, const int32_t* slot_idx, const int32_t* seq_offsets,
-                                  int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, float softmax_scale,
-                                  void* workspace, size_t workspace_bytes, hipStream_t stream, DecodePartials* out) {
+esp_status launch_decode(const void* q, const void* k_pool, const void* v_pool, const int32_t* slot_idx,
+                         const int32_t* seq_offsets, int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq,
+                         int32_t Hkv, float softmax_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream, const MergeArgs* peers, int32_t n_peers) {
+    if (decode_whole(B, total_tokens, max_len, Hq, Hkv))
+        return launch_decode_whole(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, Hq, Hkv, decode_burst_layout(Hq, Hkv),
+                                   softmax_scale * kLog2e, O, LSE, peers, n_peers, stream);
+    if ((int64_t)B * Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode: too many rows for one launch");
+    const int32_t pairs = B * Hq;
     DecodeGeom g = decode_geom(B, total_tokens, Hq, Hkv, workspace_bytes);
     const int32_t parts = decode_parts(g, B, max_len, Hq, Hkv);
     size_t n = decode_slots(g, B) * (size_t)Hq;
     float* part_acc = (float*)workspace;
     float* part_ml = part_acc + n * kHeadDim;
-    *out = DecodePartials{g.range, parts, part_acc, part_ml};
     const int G = Hq / Hkv;
     if (total_tokens > 0 && g.nhb_wg == 0) {
         esp_status st = launch_decode_gq(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, g.range, parts, g.nwg, Hq, Hkv,
@@ -576,27 +582,11 @@ esp_status launch_decode_partials(const void* q, const void* k_pool, const void*
         esp_status st = check_launch("decode_partial_kernel");
         if (st != ESP_OK) return st;
     }
-    return ESP_OK;
-}
-
-esp_status launch_decode(const void* q, const void* k_pool, const void* v_pool, const int32_t* slot_idx,
-                         const int32_t* seq_offsets, int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq,
-                         int32_t Hkv, float softmax_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes,
-                         hipStream_t stream, const MergeArgs* peers, int32_t n_peers) {
-    if (decode_whole(B, total_tokens, max_len, Hq, Hkv))
-        return launch_decode_whole(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, Hq, Hkv, decode_burst_layout(Hq, Hkv),
-                                   softmax_scale * kLog2e, O, LSE, peers, n_peers, stream);
-    if ((int64_t)B * Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode: too many rows for one launch");
-    const int32_t pairs = B * Hq;
-    DecodePartials p;
-    const esp_status st = launch_decode_partials(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, max_len, Hq, Hkv, softmax_scale,
-                                                 workspace, workspace_bytes, stream, &p);
-    if (st != ESP_OK) return st;
     const bool with_peers = peers != nullptr && n_peers > 0;
-    const bool wave = (int64_t)max_len / p.range + 2 <= kCombineShort;
+    const bool wave = (int64_t)max_len / g.range + 2 <= kCombineShort;
 #define ESP_COMBINE_LAUNCH(GROUPS, PEERS)                                                                                 \
     hipLaunchKernelGGL((decode_combine_kernel<GROUPS, PEERS>), row_grid(((int64_t)pairs + 8 / GROUPS - 1) / (8 / GROUPS)), dim3(256), 0, \
-                       stream, seq_offsets, p.range, p.parts, Hq, pairs, p.acc, p.ml,        \
+                       stream, seq_offsets, g.range, parts, Hq, pairs, (const float*)part_acc, (const float*)part_ml,        \
                        with_peers ? *peers : MergeArgs{}, n_peers, (U32x2*)O, LSE)
     if (wave && with_peers) ESP_COMBINE_LAUNCH(2, true);
     else if (wave) ESP_COMBINE_LAUNCH(2, false);

@@ -26,6 +26,8 @@ static_assert(kSharedWaves * kSharedTile <= 2 * kSharedHalf && kSharedWaves * kC
 // probabilities change nothing for their bf16 or the fp32 sums.
 constexpr float kSharedSum = 4096.f;
 
+// Partials of ranges of `range` keys: accumulators [slots][rows][128], then (maximum, sum) pairs [slots][rows]; those of list b, whose first token is s0, lie
+// from slot s0 / range + b on.  Rows: max_group Hq of a prefix, Hq of a request.
 struct SharedParts { float* acc; float* ml; int32_t range; };
 // The work of the first launch: `prefix` workgroups on the prefix (units (range, KV head), `blocks` column blocks each) and `own` on the requests' own
 // rows, in eights, spread evenly among each other.
@@ -119,8 +121,8 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
 }
 
 // The requests' own rows: a wavefront alone on (a range of a request, KV head, up to 32 of its query heads), heads next to each other as in a
-// pool row; its partial goes to the plain decode's slot of that range.
-__device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2, const DecodePartials& mine, int32_t index, unsigned char* smem, int wave, int lane) {
+// pool row; its partial goes to that range's slot.
+__device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2, const SharedParts& mine, int32_t index, unsigned char* smem, int wave, int lane) {
     const int qi = lane & 31, hi = lane >> 5;
     const int G = a.Hq / a.Hkv, chunks = (G + 31) / 32;
     const uint32_t unit = (uint32_t)index * kSharedWaves + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
@@ -146,13 +148,13 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
     const float l = half_swap_sum(cols.l), l_r = half_swap_sum(cols.l_r), fix = l_r > 0.f ? l / l_r : 0.f;
     if (qi >= ng) return;
     const int64_t ph = (int64_t)(at.w + at.b) * a.Hq + h0 + qi;
-    float* dst = const_cast<float*>(mine.acc) + ph * kHeadDim + 4 * hi;
+    float* dst = mine.acc + ph * kHeadDim + 4 * hi;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
             *(float4*)(dst + 32 * db + 2 * r) = make_float4(cols.oacc[db][r] * fix, cols.oacc[db][r + 1] * fix, cols.oacc[db][r + 2] * fix, cols.oacc[db][r + 3] * fix);
-    if (hi == 0) *(float2*)(const_cast<float*>(mine.ml) + ph * 2) = make_float2(cols.m, l);
+    if (hi == 0) *(float2*)(mine.ml + ph * 2) = make_float2(cols.m, l);
 }
 
 // The prefix.  A workgroup of eight wavefronts has COLS tiles of 32 columns, a wavefront one, and the COLS wavefronts that have different
@@ -406,7 +408,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
 // Column tiles of a workgroup on the prefix of a group with so many packed rows.
 __host__ __device__ __forceinline__ int shared_cols(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
 
-__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, DecodePartials mine, SharedWork work) {
+__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, SharedParts mine, SharedWork work) {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedLds];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -523,7 +525,7 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(Shar
 // Combination, as the plain decode's (decode.hip): groups of 32 lanes take a pair's partials in turn, four at a time, first those of the
 // prefix, then its own.
 template <int GROUPS>
-__global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32_t pairs, SharedParts parts, DecodePartials mine) {
+__global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32_t pairs, SharedParts parts, SharedParts mine) {
     constexpr int U = 4;
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     const int64_t at = row_block() * (8 / GROUPS) + grp / GROUPS;
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
         }
         break;
     }
-    if (s1 > s0) add(mine.acc, mine.ml, ((int64_t)(s0 / mine.range) + b) * a.Hq + h, a.Hq, own_partials(s0, s1, mine.range, mine.parts));
+    if (s1 > s0) add(mine.acc, mine.ml, ((int64_t)(s0 / mine.range) + b) * a.Hq + h, a.Hq, (s1 - s0 - 1) / mine.range + 1);
 
     float mx, Lt = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     if (GROUPS == 2) {
@@ -697,7 +699,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     float* const acc = (float*)workspace;
     const SharedParts parts = {acc, acc + p.slots * a.max_group * a.Hq * kHeadDim, p.range};
     float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
-    const DecodePartials mine = {p.own_range, -1, own_acc, own_acc + p.own_slots * a.Hq * kHeadDim};
+    const SharedParts mine = {own_acc, own_acc + p.own_slots * a.Hq * kHeadDim, p.own_range};
     const SharedWork work = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks};
     hipLaunchKernelGGL(shared_partial_kernel, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
     const esp_status st = check_launch("shared_partial_kernel");

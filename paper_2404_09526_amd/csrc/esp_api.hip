@@ -404,11 +404,14 @@ esp_status esp_partial_attn_decode_shared(const void* q, const void* k_pool, con
     return launch_decode_shared(a, workspace, (hipStream_t)stream);
 }
 
-// an output that shares memory with its input without being it
+// an output that shares memory with its input without being it (rows next to the input's, in the same buffer, share none)
 static bool halfway(const void* out, int64_t out_stride, const void* in, int64_t in_stride, int64_t T, int64_t row) {
     if (out == in && out_stride == in_stride) return false;
     const char *a = (const char*)out, *b = (const char*)in;
-    return a < b + ((T - 1) * in_stride + row) * 2 && b < a + ((T - 1) * out_stride + row) * 2;
+    if (a >= b + ((T - 1) * in_stride + row) * 2 || b >= a + ((T - 1) * out_stride + row) * 2) return false;
+    if (out_stride != in_stride) return true;
+    const int64_t apart = (a - b) / 2 % in_stride, from = apart < 0 ? apart + in_stride : apart;   // of an output row from the input row before it
+    return from < row || in_stride - from < row;
 }
 
 esp_status esp_qk_norm_rope_append(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,

@@ -88,18 +88,6 @@ esp_status launch_build_slots(const int32_t* table, int32_t rows, int32_t width,
                               const int32_t* lens, int32_t B, int32_t keep_first, int32_t keep_last, int32_t pos_first, int32_t pos_stride,
                               int32_t capacity, int32_t* seq_offsets, int32_t* slots, int32_t* pos, hipStream_t stream);
 
-// The partials of a decode call in ranges, on their way to a combination: those of a request begin at slot s0 / range + b (s0: its first
-// token) and are as many as own_partials says; accumulators [slots][Hq][128], then (maximum, sum) pairs [slots][Hq].
-struct DecodePartials { int32_t range, parts; const float* acc; const float* ml; };
-__device__ __forceinline__ int own_partials(int32_t s0, int32_t s1, int32_t range, int32_t parts) {
-    const int whole = (s1 - s0 - 1) / range + 1;
-    return parts == 0 ? (s1 - 1) / range - s0 / range + 1 : parts > 0 ? min(parts, whole) : whole;
-}
-esp_status launch_decode_partials(const void* q, const void* k_pool, const void* v_pool, const int32_t* slot_idx, const int32_t* seq_offsets,
-                                  int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, float softmax_scale,
-                                  void* workspace, size_t workspace_bytes, hipStream_t stream, DecodePartials* out);
-int32_t decode_range(int32_t total_tokens, int64_t step, int64_t least, int64_t rows, int64_t kept, int64_t room);
-
 // decode behind shared prefixes (decode_shared.hip)
 struct SharedArgs {
     const void* q; const char* k_pool; const char* v_pool;

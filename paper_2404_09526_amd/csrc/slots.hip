@@ -6,6 +6,9 @@
 // Both are a prefix sum over the requests and then a map over its total, all elements alike; with a few hundred requests what counts is
 // the chain of round trips, so both are one launch: every workgroup takes the prefix sum itself (the lengths are a few KB in the L2),
 // 1024 requests at a time, and then its share of the elements.
+// Measured: the pages of 64 requests' next tokens 4.6 us, the slots of 16 requests of some 600 tokens 4.8 us, hardly more than an empty launch.  Long lists are
+// bound by their bytes, written and of the table: 256 lists of 7.2 M slots in all, pages of one (57.5 MB), took 34 us with one slot a thread, with four, whole pieces
+// of 16 bytes, 15.6 us, 3.7 TB/s.
 #include "esp_common.h"
 
 namespace esp {
@@ -212,7 +215,8 @@ static unsigned slot_grid(int64_t elements) {
 
 esp_status launch_extend_table(const int32_t* free_pages, int32_t n_free, const int32_t* req_row, const int32_t* old_lens, const int32_t* new_lens,
                                int32_t B, int32_t page, int32_t* table, int32_t rows, int32_t width, int32_t* taken, hipStream_t stream) {
-    // (how many pages there are to place is not known here; a workgroup that finds none for it ends after the prefix sum)
+    // (how many pages there are to place is not known here; a workgroup that finds none for it ends after the prefix sum.  So there are at most two to a CU:
+    // a step has few new pages, and of a list that is longer each takes several chunks.)
     const int64_t most = (int64_t)B * width < n_free ? (int64_t)B * width : n_free;
     hipLaunchKernelGGL(extend_table_kernel, dim3(slot_grid(most) < 512 ? slot_grid(most) : 512), dim3(kSlotThreads), 0, stream, free_pages, n_free, req_row,
                        old_lens, new_lens, B, page, table, rows, width, taken);

@@ -253,6 +253,21 @@ def test_norm_of_zeros_and_of_the_largest_values(cuda):
     assert (q[0] == 0).all() and (q[1] == 1).all()
 
 
+def test_new_queries_go_next_to_the_old_ones(cuda):
+    """q_out may be other columns of the buffer that q is columns of: the rows share nothing, though the two spans do."""
+    gen = torch.Generator(device=cuda).manual_seed(3)
+    rows = torch.randn((37, 20, 128), generator=gen, device=cuda).bfloat16()
+    k = torch.randn((37, 2, 128), generator=gen, device=cuda).bfloat16()
+    pos, freq = i32(np.arange(37), cuda), torch.tensor(1e4 ** (-np.arange(64) / 64), dtype=torch.float32, device=cuda)
+    want, _, _ = esp.esp_qk_norm_rope_append(rows[:, 4:12], k, k, pos, freq)
+    was = rows.clone()
+    esp.esp_qk_norm_rope_append(rows[:, 4:12], k, k, pos, freq, q_out=rows[:, 12:])
+    assert torch.equal(rows[:, 12:], want) and torch.equal(rows[:, :12], was[:, :12])
+    for at in (0, 5, 11):                                              # over some of their heads
+        with pytest.raises(esp.EspError, match="overlaps"):
+            esp.esp_qk_norm_rope_append(rows[:, 4:12], k, k, pos, freq, q_out=rows[:, at:at + 8])
+
+
 def test_rotation_of_no_tokens(cuda):
     x, y = torch.empty((0, 8, 128), dtype=torch.bfloat16, device=cuda), torch.empty((0, 2, 128), dtype=torch.bfloat16, device=cuda)
     assert esp.esp_qk_norm_rope_append(x, y, y)[0].shape == (0, 8, 128)
@@ -312,6 +327,8 @@ SHARED = [
     ("columns-33", [11], [700], [3] * 11, 6, 2), ("columns-64", [16], [900], [8] * 16, 32, 8), ("columns-65", [65], [333], [2] * 65, 4, 4), ("columns-128", [32], [800], [5] * 32, 32, 8),
     ("columns-200", [50], [1031], [1] * 50, 32, 8), ("columns-256", [64], [513], [7] * 64, 32, 8), ("columns-257", [257], [290], [0] * 257, 2, 2),
     ("columns-600", [150, 4], [777, 3000], [1] * 154, 8, 2), ("ragged-groups", [1, 90, 2], [4000, 33, 2100], [17] * 93, 32, 4), ("long", [2], [20000], [500, 3], 8, 2),
+    ("many-groups", [1, 0, 2] * 50, [40, 7, 65] * 50, [5, 0, 33] * 50, 4, 2), ("many-requests", [699, 1], [120, 600], [0, 3, 70, 1, 600, 9, 33] * 100, 4, 1),
+    ("many-of-both", [3] * 300, [1, 200, 0] * 100, [2, 0, 35] * 300, 2, 2),
 ]
 
 
@@ -389,6 +406,40 @@ def test_shared_scores_far_apart(cuda, form):
         Or, Lr = shared_reference(call, both, cuda)
         O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=shared_workspace(call, cuda))
         check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), at)
+
+
+@pytest.fixture
+def validating(cuda):
+    was = esp.esp_debug_set_validate(True)
+    yield
+    esp.esp_debug_set_validate(was)
+
+
+def test_what_the_debugging_checks_look_at(cuda, validating):
+    """Refused on the host, before anything runs: slots outside the pool, offsets that decrease or end elsewhere, pieces longer than stated, rows and slots
+    named twice."""
+    call, _ = shared_inputs(cuda, [3, 2], [200, 90], [5, 0, 7, 9, 1], 8, 2, 5)
+    esp.esp_partial_attn_decode_shared(**call)
+    for name, values in (("prefix_slots", {7: 1 << 20}), ("prefix_slots", {289: -1}), ("slot_idx", {21: 1 << 20}), ("prefix_offsets", {1: 291}), ("prefix_offsets", {1: 80}),
+                         ("prefix_offsets", {2: 289}), ("group_offsets", {1: 6}), ("group_offsets", {2: 4}), ("seq_offsets", {5: 21}), ("seq_offsets", {0: 1})):
+        bad = call[name].clone()
+        for i, x in values.items():
+            bad[i] = x
+        with pytest.raises(esp.EspError):
+            esp.esp_partial_attn_decode_shared(**dict(call, **{name: bad}))
+    x = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device=cuda)
+    pools = [torch.zeros((8, 2, 128), dtype=torch.bfloat16, device=cuda) for _ in range(2)]
+    esp.esp_qk_norm_rope_append(x, x, x, slot_idx=i32([3, -1, 2], cuda), k_pool=pools[0], v_pool=pools[1])
+    with pytest.raises(esp.EspError, match="twice"):
+        esp.esp_qk_norm_rope_append(x, x, x, slot_idx=i32([3, 1, 3], cuda), k_pool=pools[0], v_pool=pools[1])
+    table, lens = torch.full((4, 3), -1, dtype=torch.int32, device=cuda), i32([1, 2], cuda)
+    esp.esp_extend_block_table(table, i32([5, 6], cuda), i32([0, 0], cuda), lens, 4, req_row=i32([3, 1], cuda))
+    esp.esp_build_slots(table, lens, 4, req_row=i32([3, 3], cuda), capacity=8)
+    for rows in ([3, 3], [0, 4], [-1, 0]):
+        with pytest.raises(esp.EspError):
+            esp.esp_extend_block_table(table, i32([5, 6], cuda), i32([0, 0], cuda), lens, 4, req_row=i32(rows, cuda))
+    with pytest.raises(esp.EspError):
+        esp.esp_build_slots(table, lens, 4, req_row=i32([0, 4], cuda), capacity=8)
 
 
 # ----------------------------------------------------------------------------------------------------------- all of them together

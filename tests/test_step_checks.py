@@ -52,6 +52,8 @@ def test_norm_and_rotation(lib):
         assert call(**kw) == bad, kw
     assert call(q_out=P((1 << 24) + 2048)) == bad and "overlaps" in lib.last_error()      # the next token's queries
     assert call(q_out=far["q"], qos=2048) == bad                       # itself, but with other strides
+    assert call(q_out=P((1 << 24) + 2032), qs=2048, qos=2048) == bad   # eight elements short of the place next to it, or past it
+    assert call(q_out=P((1 << 24) - 2032), qs=2048, qos=2048) == bad and call(q_out=P((1 << 24) + 2064), qs=2048, qos=2048) == bad
     assert call(k_out=far["k"], ks=512) == bad and call(v_out=P((1 << 26) + 16)) == bad
 
 
