@@ -30,8 +30,16 @@ constexpr float kSharedSum = 4096.f;
 // from slot s0 / range + b on.  Rows: max_group Hq of a prefix, Hq of a request.
 struct SharedParts { float* acc; float* ml; int32_t range; };
 // The work of the first launch: `prefix` workgroups on the prefix (units (range, KV head), `blocks` column blocks each) and `own` on the requests' own
-// rows, in eights, spread evenly among each other.
-struct SharedWork { int32_t prefix, own, units, blocks; };
+// rows, in eights: among the first `first` eights first_prefix are the prefix's, up to number `mixed` the rest of those, spread evenly both times; own rows alone
+// come last.
+struct SharedWork {
+    int32_t prefix, own, units, blocks, first, first_prefix, mixed;
+    __device__ __forceinline__ uint32_t before(uint32_t eight) const {   // eights of the prefix among the first so many
+        const uint32_t all = (uint32_t)prefix >> 3, n = first, of_n = first_prefix, m = mixed;
+        if (eight < n) return (uint64_t)eight * of_n / n;
+        return eight < m ? of_n + (uint64_t)(eight - n) * (all - of_n) / (m - n) : all;
+    }
+};
 
 // A wavefront on tiles of 32 keys of its own, number `first`, first + step, ...: their rows go to its block of the LDS, the next tile's K as soon
 // as this one's scores are taken, its V as soon as this one's has been read.  list: the slots of all `seg` keys, in LDS (a load of them on the way would
@@ -340,6 +348,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
             meet();
             // (past the last step there is nothing to read: what is there instead is never used)
             if (n_rows > 0) {
+                __builtin_amdgcn_s_setprio(1);                      // (the other wavefront's vector instructions take what these leave, not the other way round)
                 const uint32_t k_next = k_tile(i + 2), v_next = v_tile(i + 1);
                 zero();
 #pragma unroll
@@ -350,6 +359,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
                     read_v(v_next, t);
                     __builtin_amdgcn_sched_barrier(0);              // (in this order: the chain of the scores beside the sums of V, an operand's place taken over at once)
                 }
+                __builtin_amdgcn_s_setprio(0);
             }
             // every wavefront is done with the products of the step before this one, and with what they read
             fetch_group(i + STAGES);
@@ -413,8 +423,7 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(Sh
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the eight that this workgroup is of, and how many before it are the prefix's: the workgroups of an eight lie on all XCDs in turn
-    const uint32_t eight = blockIdx.x >> 3, of = blockIdx.x & 7, prefix = work.prefix >> 3, all = (work.prefix + work.own) >> 3;
-    const uint32_t before = (uint64_t)eight * prefix / all, after = (uint64_t)(eight + 1) * prefix / all;
+    const uint32_t eight = blockIdx.x >> 3, of = blockIdx.x & 7, before = work.before(eight), after = work.before(eight + 1);
     if (after == before) {
         shared_own(a, scale_log2, mine, (eight - before) * 8 + of, smem, wave, lane);
         return;
@@ -611,6 +620,7 @@ struct SharedPlan {
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
     double us;                                                      // the estimate
     int kind;                                                       // column tiles of a workgroup for an average group, 2^kind
+    double share, last;                                             // the prefix's share of the time of all workgroups; a workgroup of it, of the whole launch
 };
 // One workgroup a CU, whichever kind.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least: a workgroup
 // on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and a third
@@ -641,7 +651,10 @@ static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total,
             double us = fmax(fmax(sum / kCus + kTail * longest, longest), memory);
             if (n <= kFewRounds * kCus) us = fmax(us, kWholeRound * ceil(n / kCus) * sum / n);
             us += wgs * cols * kPartial;
-            if (us < best_us) { best_us = us; p.range = range; p.own_range = own_range; }
+            if (us < best_us) {
+                best_us = us; p.range = range; p.own_range = own_range;
+                p.share = prefix_us / sum; p.last = one / (sum / kCus);
+            }
             if (total_tokens == 0) break;
         }
         if (range >= prefix_total) break;
@@ -679,6 +692,32 @@ static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
     return whole < 0.95 * ranges;
 }
 
+// The order of the first launch.  Workgroups start in the order of their numbers as others end (on each XCD, and there on one shader engine after the other:
+// one that is full holds up what comes behind).  What ends last should be short, and the prefix's workgroups are the long ones: so of those that start together as
+// many are the prefix's as its share of the time, the rest follow evenly, and own rows alone fill the time that the last of the prefix take, and half as much
+// again (their last ranges are short).  A prefix with few columns is bound by the memory as own rows are, nothing is gained side by side, and it comes first.
+// Evenly mixed -> so: 96 + 100 + 60 requests behind 66, 40 and 20 thousand tokens, 32 / 8 heads, 442 -> 418 us; 1 + 110 + 12 behind 12452, 947 and 28, 32 / 8, 71 -> 56;
+// 16 behind 65536, 32 / 32, 243 -> 234.  Up to 1.6 rounds of the chip it matters which ones the second gets, and evenly mixed is the better: 25 + 38 behind 16464 and
+// 4705, 32 / 4, 48.6 against 53.1.  (Workgroups that take one piece of work after another by a counter: 416, and their loop costs others 4 % in the mean.)
+static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own) {
+    SharedWork w = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks, 0, 0, 0};
+    const int32_t P = w.prefix >> 3, N = w.own >> 3, all = P + N, round = 32;
+    if (all * 5 <= round * 8) {
+        w.first = w.mixed = all;
+        w.first_prefix = P;
+    } else if (p.kind <= 1) {
+        w.first = w.first_prefix = w.mixed = P;
+    } else {
+        w.first = round;
+        w.first_prefix = (int32_t)lround(round * p.share);
+        if (w.first_prefix < round - N) w.first_prefix = round - N;
+        if (w.first_prefix > P) w.first_prefix = P;
+        w.mixed = all - (int32_t)(N * fmin(1.0, 1.5 * p.last));
+        if (w.mixed < round + P - w.first_prefix) w.mixed = round + P - w.first_prefix;
+    }
+    return w;
+}
+
 esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_t stream) {
     if (a.prefix_total == 0 || a.max_group == 0)
         return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
@@ -700,7 +739,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     const SharedParts parts = {acc, acc + p.slots * a.max_group * a.Hq * kHeadDim, p.range};
     float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
     const SharedParts mine = {own_acc, own_acc + p.own_slots * a.Hq * kHeadDim, p.own_range};
-    const SharedWork work = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks};
+    const SharedWork work = shared_order(p, prefix, own);
     hipLaunchKernelGGL(shared_partial_kernel, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
     const esp_status st = check_launch("shared_partial_kernel");
     if (st != ESP_OK) return st;
