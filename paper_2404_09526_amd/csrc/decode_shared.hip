@@ -622,14 +622,16 @@ struct SharedPlan {
     int kind;                                                       // column tiles of a workgroup for an average group, 2^kind
     double share, last;                                             // the prefix's share of the time of all workgroups; a workgroup of it, of the whole launch
 };
+// Rounds of the chip from which on the order is not an even mixture (shared_order).
+constexpr double kOneAfter = 1.6;
 // One workgroup a CU, whichever kind.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least: a workgroup
-// on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and a third
-// of the longest at the end, or, where they are only a few rounds of the chip, whole rounds; the longest alone; all rows at the memory's rate.  What is not
-// known is how the groups differ: several are taken to be as large as their average.  Measured on 92 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of
-// 0 .. 110000 tokens, thirteen head layouts) with 66 choices each, the estimates' choice was 5.6 % from the best on average; with the largest group in
-// place of the average 7.3 %, with one fixed choice for all (512 and 128) 21 %.
+// on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and at the end
+// a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip, whole rounds; the longest alone; all rows at the
+// memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.  Measured on 98 batches (1 .. 250 requests in
+// 1 .. 5 groups, prefixes of 0 .. 110000 tokens, thirteen head layouts) the estimates' choice in that order took 0.8 % less than the best of 66 choices for each
+// evenly mixed, which it was 5.6 % from there (with the largest group in place of the average 7.3 %, with one fixed choice for all, 512 and 128, 21 %).
 static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 3.3, kTail = 0.33, kFewRounds = 2.5, kWholeRound = 1.2, kPartial = 0.0105, kBytesPerUs = 6.4e6;
+    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 3.3, kTail = 0.33, kTailBoth = 0.2, kFewRounds = 2.5, kWholeRound = 1.2, kPartial = 0.0105, kBytesPerUs = 6.4e6;
     struct Times { double start, step; };
     constexpr Times kTimes[4] = {{7, 4.5}, {8, 2.7}, {9, 1.25}, {10, 1.15}};   // of a workgroup with 1, 2, 4, 8 column tiles
     constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
@@ -648,7 +650,9 @@ static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total,
         for (const int32_t own_range : kOwnRanges) {
             const double own = (double)own_wgs(own_range), longest = total_tokens == 0 ? one : fmax(one, kOwnStart + kOwnTile * own_range / 32);
             const double sum = prefix_us + own * kOwnStart + own_tiles * kOwnTile, n = wgs + own;
-            double us = fmax(fmax(sum / kCus + kTail * longest, longest), memory);
+            const double mine = kOwnStart + kOwnTile * own_range / 32;
+            const double ends = own == 0 || n <= kOneAfter * kCus ? kTail * longest : kind <= 1 ? kTail * mine : kTailBoth * (mine + one);
+            double us = fmax(fmax(sum / kCus + ends, longest), memory);
             if (n <= kFewRounds * kCus) us = fmax(us, kWholeRound * ceil(n / kCus) * sum / n);
             us += wgs * cols * kPartial;
             if (us < best_us) {
@@ -702,7 +706,7 @@ static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
 static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own) {
     SharedWork w = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks, 0, 0, 0};
     const int32_t P = w.prefix >> 3, N = w.own >> 3, all = P + N, round = 32;
-    if (all * 5 <= round * 8) {
+    if (all <= kOneAfter * round) {
         w.first = w.mixed = all;
         w.first_prefix = P;
     } else if (p.kind <= 1) {
