@@ -531,7 +531,8 @@ esp_status esp_fit_prefill_model(
  *   esp_debug_set_decode_plan: 1 makes every decode call of the CALLING THREAD work in
  *     ranges of the token list and combine them in a second launch, 2 in one launch, a
  *     workgroup to a request and key-value head; by default (0, and anything else) that
- *     too follows from an estimate.  For tests as well.
+ *     too follows from an estimate.  Decode behind shared prefixes goes by it as well.  For
+ *     tests.
  * and, changing nothing,
  *   esp_debug_prefill_plan_for: what a call of these sizes, with or without a causal
  *     mask, that keeps rows in the pool or not, with such a workspace would run on now,
