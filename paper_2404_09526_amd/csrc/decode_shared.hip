@@ -5,7 +5,11 @@
 //   S^T [keys x columns] = K Q^T,   O^T [128 x columns] += V^T P^T
 // against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row).  With few columns the prefix is bound by the
 // memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
-// ranges side by side, and what bounds the one is left over by the other.  A second launch combines the partials of both kinds.
+// ranges side by side, and what bounds the one is left over by the other (shared_order).  A second launch combines the partials of both kinds.
+// Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes of many columns, which
+// read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
+// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 51 us (207 MB); 16 behind 65536, 32 / 32, 222 (1.24 GB, 5.6 TB/s); 256 in three groups behind 65549,
+// 40000 and 20011, 32 / 8, 420 (1.59 GB and 193 GFLOP); four short requests 7.5.
 #include <math.h>
 
 #include "column_tile.h"
@@ -13,14 +17,18 @@
 
 namespace esp {
 
-constexpr int kSharedWaves = 8;
 constexpr int kSharedTile = kColKBytes + kColVBytes;
-constexpr int kSharedHalf = 64 * 1024;
-constexpr int kSharedMost = 4096;                                   // keys of a prefix range: its slots lie in LDS
-constexpr int kSharedOwn = kSharedMost / kSharedWaves;              // keys of an own range, a wavefront's
-constexpr int kSharedLds = 2 * kSharedHalf + kSharedMost * 4;
-// tiles that wavefronts have for themselves lie before the lists; the blocks of the combination, which are larger, may lie on them: it comes last
-static_assert(kSharedWaves * kSharedTile <= 2 * kSharedHalf && kSharedWaves * kColWaveBytes <= kSharedLds, "the wavefronts' tiles and blocks fit");
+// A workgroup of the first launch has four wavefronts, two of them share a CU, or eight, which have it alone.
+template <int WAVES>
+struct SharedGeometry {
+    static constexpr int half = WAVES * (kSharedTile / 2), most = WAVES * 512;   // of the tiles' LDS; keys of a prefix range: its slots lie in LDS
+    static constexpr int own = 512;                                 // keys of an own range, a wavefront's: its slots too
+    static constexpr int lds = 2 * half + most * 4;
+    // tiles that wavefronts have for themselves lie before the lists; the blocks that rows are stored from, which are larger, may lie on them: they come last
+    static_assert(WAVES * kSharedTile <= 2 * half && WAVES * (kColWaveBytes + 32 * 8) <= lds && WAVES * own <= most, "the wavefronts' tiles and blocks fit");
+    static_assert(lds <= 16 * 1024 * 10 * WAVES / 8, "two of four, or one of eight, on a CU");
+};
+constexpr int kWholeWaves = 8;                                      // of a workgroup of the one-launch form
 // The offset that a wide workgroup takes probabilities against is moved (and the accumulators with it) only where those of a tile sum up to more than
 // this: moved with every new maximum, as the plain decode's, it moves in half of the tiles for some column of the 32.  Larger
 // probabilities change nothing for their bf16 or the fp32 sums.
@@ -130,16 +138,17 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
 
 // The requests' own rows: a wavefront alone on (a range of a request, KV head, up to 32 of its query heads), heads next to each other as in a
 // pool row; its partial goes to that range's slot.
+template <int WAVES>
 __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2, const SharedParts& mine, int32_t index, unsigned char* smem, int wave, int lane) {
     const int qi = lane & 31, hi = lane >> 5;
     const int G = a.Hq / a.Hkv, chunks = (G + 31) / 32;
-    const uint32_t unit = (uint32_t)index * kSharedWaves + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
+    const uint32_t unit = (uint32_t)index * WAVES + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
     const int kvh = rest / (uint32_t)chunks, g0 = (rest - kvh * chunks) * 32, ng = min(32, G - g0), h0 = kvh * G + g0;
     int32_t none;
     const RequestRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, lane, nullptr, none, none);
     const int32_t seg = min(at.t1, a.total_tokens) - at.t0;         // (never past the slot list)
     if (seg <= 0) return;
-    int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf) + wave * kSharedOwn;
+    int32_t* const list = (int32_t*)(smem + 2 * SharedGeometry<WAVES>::half) + wave * SharedGeometry<WAVES>::own;
     for (int j = lane; j < seg; j += 64) list[j] = a.slot_idx[at.t0 + j];
     bf16x8 qf[8];
     const int64_t row = (int64_t)at.b * a.Hq + h0 + min(qi, ng - 1);
@@ -165,20 +174,21 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
     if (hi == 0) *(float2*)(mine.ml + ph * 2) = make_float2(cols.m, l);
 }
 
-// The prefix.  A workgroup of eight wavefronts has COLS tiles of 32 columns, a wavefront one, and the COLS wavefronts that have different
-// columns (a team) share tiles of 32 keys in LDS, so that a row of K and V comes from memory once for 32 COLS columns; the 8 / COLS teams take
+// The prefix.  A workgroup has COLS tiles of 32 columns, a wavefront one, and the COLS wavefronts that have different
+// columns (a team) share tiles of 32 keys in LDS, so that a row of K and V comes from memory once for 32 COLS columns; the WAVES / COLS teams take
 // the tiles in turn, all teams' tiles are a step.
 // A step of a wavefront is two phases that take about as long as each other: the scores of its tile become probabilities (vector ALU); then the
 // products, the NEXT tile's scores and this one's V, without a wait, each followed by the LDS read of the operand that takes its place
-// (matrix cores).  The two wavefronts of a SIMD are a phase apart, the barriers between phases keep them so.  K's operands are thus read two steps ahead
-// of the scores, V's one step ahead of their products, and each has a ring of COLS stages (128 KiB together): group j of transfers is V of step j
+// (matrix cores).  Of eight wavefronts the two of a SIMD are a phase apart, the barriers between phases keep them so; of four each has another workgroup's beside
+// it, and one barrier a step is enough.  K's operands are thus read two steps ahead
+// of the scores, V's one step ahead of their products, and each has a ring of COLS stages (16 KiB a wavefront together): group j of transfers is V of step j
 // and K of step j + 1.
 // A team of one wavefront shares nothing: it waits for its own rows only (sweep_tiles).
 struct PrefixPart { RequestRange at; int32_t b0, seg, n_all, kvh; };  // a range of group at.b's prefix: its keys, the group's first request and packed rows
-template <int COLS>
+template <int WAVES, int COLS>
 __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, const PrefixPart& part, uint32_t cb, unsigned char* smem,
                                               int wave, int lane) {
-    constexpr int TEAMS = kSharedWaves / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
+    constexpr int TEAMS = WAVES / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
     const int team = wave / COLS, ct = wave % COLS;
     const int qi = lane & 31, hi = lane >> 5;
     const RequestRange& at = part.at;
@@ -186,8 +196,8 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
     if (n_all <= (int32_t)cb * (32 * COLS)) return;
     const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = n_all - rho0;   // (columns of this wavefront, up to 32; none: it only moves tiles)
 
-    int32_t* const list = (int32_t*)(smem + 2 * kSharedHalf);
-    for (int i = threadIdx.x; i < seg; i += kSharedWaves * 64) list[i] = a.prefix_slots[t0 + i];
+    int32_t* const list = (int32_t*)(smem + 2 * SharedGeometry<WAVES>::half);
+    for (int i = threadIdx.x; i < seg; i += WAVES * 64) list[i] = a.prefix_slots[t0 + i];
 
     // row of this column within the group's queries (past the last: the last one's, whose results are not written)
     const int32_t rho = min(rho0 + qi, n_all - 1), of = rho / G;
@@ -207,12 +217,13 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
     __syncthreads();                                                // the list is there
     if constexpr (COLS == 1) {
         cols.place(lds + wave * kSharedTile, lane);
-        sweep_tiles(cols, qf, lds + wave * kSharedTile, kbase, vbase, row_bytes, wave, kSharedWaves, seg, list, scale_log2, lane);
+        sweep_tiles(cols, qf, lds + wave * kSharedTile, kbase, vbase, row_bytes, wave, WAVES, seg, list, scale_log2, lane);
     } else {
+        constexpr bool PHASES = WAVES == 8;
         constexpr int STAGES = COLS, kTile = kColKBytes;            // of K; V's is as large
         constexpr int kRing = STAGES * TEAMS * kTile;
-        static_assert(2 * kRing == 2 * kSharedHalf, "both rings end where the list begins");
-        const bool late = wave >= kSharedWaves / 2;                 // (wavefronts w and w + 4 are on one SIMD)
+        static_assert(2 * kRing == 2 * SharedGeometry<WAVES>::half, "both rings end where the list begins");
+        const bool late = PHASES && wave >= WAVES / 2;                 // (wavefronts w and w + 4 are on one SIMD)
         const int steps = (seg + STEP - 1) / STEP;
         auto k_tile = [&](int i) { return lds + ((i % STAGES) * TEAMS + team) * kTile; };
         auto v_tile = [&](int i) { return lds + kRing + ((i % STAGES) * TEAMS + team) * kTile; };
@@ -364,14 +375,15 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
             // every wavefront is done with the products of the step before this one, and with what they read
             fetch_group(i + STAGES);
             if (late) landed(i + 1);
-            meet();
+            if (PHASES) meet();
         }
-        if (!late) meet();
+        if (PHASES && !late) meet();
     }
     // The wavefronts leave their columns as rows of 128 (and 4 of padding) floats in LDS, maxima and sums behind them; then every wavefront combines
     // the teams' rows and stores its share of them, 32 lanes a row.  (Stored from the accumulators, 16 bytes of 32 rows at a time, 256 such blocks took 11 us.)
     constexpr int kPitch = kHeadDim + 4;
-    static_assert(32 * kPitch * 4 <= kColWaveBytes && kSharedWaves * (kColWaveBytes + 32 * 8) <= kSharedLds, "the rows fit");
+    constexpr int kRowPairs = 16 * COLS / WAVES;                    // of a wavefront
+    static_assert(32 * kPitch * 4 <= kColWaveBytes, "the rows fit");
     __syncthreads();                                                // the tiles are read
     {
         const float l = half_swap_sum(cols.l), l_r = half_swap_sum(cols.l_r), fix = l_r > 0.f ? l / l_r : 0.f;   // (the rounded probabilities were multiplied)
@@ -381,13 +393,13 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *(float4*)(mine + 32 * db + 2 * r) = make_float4(cols.oacc[db][r] * fix, cols.oacc[db][r + 1] * fix, cols.oacc[db][r + 2] * fix, cols.oacc[db][r + 3] * fix);
-        if (hi == 0) ((float2*)(smem + kSharedWaves * kColWaveBytes))[wave * 32 + qi] = make_float2(cols.m, l);
+        if (hi == 0) ((float2*)(smem + WAVES * kColWaveBytes))[wave * 32 + qi] = make_float2(cols.m, l);
     }
     __syncthreads();
     const int64_t slot = (int64_t)(at.w + at.b) * a.max_group * a.Hq;
 #pragma unroll 1
-    for (int i = 0; i < 2 * COLS; ++i) {
-        const int in = (wave * 2 * COLS + i) * 2 + hi;              // of the workgroup's 32 COLS columns
+    for (int i = 0; i < kRowPairs; ++i) {
+        const int in = (wave * kRowPairs + i) * 2 + hi;              // of the workgroup's 32 COLS columns
         const int32_t col = cb * (32 * COLS) + in;
         if (col >= n_all) continue;
         const int w0 = in >> 5, at_row = in & 31;                   // team t's are those of wavefront w0 + COLS t
@@ -395,7 +407,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < TEAMS; ++t) {
-            ml[t] = ((const float2*)(smem + kSharedWaves * kColWaveBytes))[(w0 + COLS * t) * 32 + at_row];
+            ml[t] = ((const float2*)(smem + WAVES * kColWaveBytes))[(w0 + COLS * t) * 32 + at_row];
             mx = fmaxf(mx, ml[t].x);
         }
         float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -415,17 +427,18 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
     }
 }
 
-// Column tiles of a workgroup on the prefix of a group with so many packed rows.
-__host__ __device__ __forceinline__ int shared_cols(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
+// Column tiles of a workgroup of so many wavefronts on the prefix of a group with so many packed rows.
+__host__ __device__ __forceinline__ int shared_cols(int64_t rows, int waves) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || waves == 4 ? 4 : 8; }
 
-__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, SharedParts mine, SharedWork work) {
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedLds];
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void shared_partial_kernel(SharedArgs a, float scale_log2, SharedParts parts, SharedParts mine, SharedWork work) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[SharedGeometry<WAVES>::lds];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the eight that this workgroup is of, and how many before it are the prefix's: the workgroups of an eight lie on all XCDs in turn
     const uint32_t eight = blockIdx.x >> 3, of = blockIdx.x & 7, before = work.before(eight), after = work.before(eight + 1);
     if (after == before) {
-        shared_own(a, scale_log2, mine, (eight - before) * 8 + of, smem, wave, lane);
+        shared_own<WAVES>(a, scale_log2, mine, (eight - before) * 8 + of, smem, wave, lane);
         return;
     }
     // Unit: (range, KV head), heads next to each other as in a pool row.  The column blocks of a unit are in eights that follow each other: on one
@@ -440,18 +453,18 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_partial_kernel(Sh
     part.n_all = min(min(b1, a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
     part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
     if (part.seg <= 0 || part.n_all <= 0) return;
-    switch (shared_cols(part.n_all)) {
-        case 1: shared_prefix<1>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        case 2: shared_prefix<2>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        case 4: shared_prefix<4>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        default: shared_prefix<8>(a, scale_log2, parts, part, cb, smem, wave, lane);
+    switch (shared_cols(part.n_all, WAVES)) {
+        case 1: shared_prefix<WAVES, 1>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 2: shared_prefix<WAVES, 2>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 4: shared_prefix<WAVES, 4>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        default: shared_prefix<WAVES, WAVES>(a, scale_log2, parts, part, cb, smem, wave, lane);
     }
 }
 
 // Few short requests, in one launch: a workgroup has one request and KV head (a chunk of its query heads) and walks the prefix and the
 // request's own rows as one list (as decode_whole.hip does with one); the prefix is read by each, from the caches, and no combination follows.
-__global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(SharedArgs a, float scale_log2) {
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[kSharedWaves * kColWaveBytes];
+__global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(SharedArgs a, float scale_log2) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[kWholeWaves * kColWaveBytes];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int qi = lane & 31, hi = lane >> 5;
@@ -476,7 +489,7 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(Shar
         return t < (uint32_t)P ? prefix[t] : own[t - P];
     };
     int32_t slots = 0, slots_next = 0;
-    if (32 * wave < n) { slots = tile_slots(wave); slots_next = tile_slots(wave + kSharedWaves); }
+    if (32 * wave < n) { slots = tile_slots(wave); slots_next = tile_slots(wave + kWholeWaves); }
     const int G = a.Hq / a.Hkv, g0 = blockIdx.z * 32, ng = min(32, G - g0);
     const uint32_t row_bytes = (uint32_t)a.Hkv * (kHeadDim * 2);
     const char* kbase = a.k_pool + (uint32_t)kvh * (kHeadDim * 2);
@@ -496,9 +509,9 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(Shar
             load_to_lds_b128_at(to + 1024 * x, base + ((uint64_t)(uint32_t)__shfl(of, col_row(x, lane)) * row_bytes + (is_k ? col_k_within(x, lane) : col_v_within(lane))));
     };
     if (32 * wave < n) { fetch(lds_k, kbase, slots, true); fetch(lds_k + kColKBytes, vbase, slots, false); }
-    for (uint32_t i = wave; 32 * i < n; i += kSharedWaves) {
+    for (uint32_t i = wave; 32 * i < n; i += kWholeWaves) {
         const int here = min(32u, n - 32 * i);
-        const bool next = 32 * (i + kSharedWaves) < n;
+        const bool next = 32 * (i + kWholeWaves) < n;
         wait_vm<8>();                                               // K has landed; V may be on its way
         floatx16 sc = cols.scores(qf);
         if (next) {
@@ -516,15 +529,15 @@ __global__ __launch_bounds__(kSharedWaves * 64, 2) void shared_whole_kernel(Shar
         cols.accumulate(pf);
         if (next) {
             fetch(lds_k + kColKBytes, vbase, slots_next, false);
-            slots_next = tile_slots(i + 2 * kSharedWaves);
+            slots_next = tile_slots(i + 2 * kWholeWaves);
         }
     }
-    constexpr int N = 64 / kSharedWaves;
+    constexpr int N = 64 / kWholeWaves;
     float out[N], mx, lsum;
-    cols.combine<kSharedWaves>(smem, wave, lane, out, mx, lsum);
+    cols.combine<kWholeWaves>(smem, wave, lane, out, mx, lsum);
     if (qi >= ng) return;
     const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;              // no token: 0; a NaN shows
-    const int at = Columns::first_element<kSharedWaves>(wave, lane);
+    const int at = Columns::first_element<kWholeWaves>(wave, lane);
 #pragma unroll
     for (int e = 0; e < N; e += 4)
         ((U32x2*)a.O)[(pair * kHeadDim + at + 2 * e) / 4] = U32x2{pack_bf16(out[e] * inv, out[e + 1] * inv), pack_bf16(out[e + 2] * inv, out[e + 3] * inv)};
@@ -619,58 +632,69 @@ struct SharedPlan {
     size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
     double us;                                                      // the estimate
-    int kind;                                                       // column tiles of a workgroup for an average group, 2^kind
+    int waves, kind;                                                // of a workgroup: wavefronts, column tiles for an average group (2^kind)
     double share, last;                                             // the prefix's share of the time of all workgroups; a workgroup of it, of the whole launch
 };
 // Rounds of the chip from which on the order is not an even mixture (shared_order).
 constexpr double kOneAfter = 1.6;
-// One workgroup a CU, whichever kind.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least: a workgroup
-// on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront; all of them together, spread evenly, and at the end
-// a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip, whole rounds; the longest alone; all rows at the
-// memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.  Measured on 98 batches (1 .. 250 requests in
-// 1 .. 5 groups, prefixes of 0 .. 110000 tokens, thirteen head layouts) the estimates' choice in that order took 0.8 % less than the best of 66 choices for each
-// evenly mixed, which it was 5.6 % from there (with the largest group in place of the average 7.3 %, with one fixed choice for all, 512 and 128, 21 %).
-static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    constexpr double kCus = 256, kOwnStart = 6, kOwnTile = 3.3, kTail = 0.33, kTailBoth = 0.2, kFewRounds = 2.5, kWholeRound = 1.2, kPartial = 0.0105, kBytesPerUs = 6.4e6;
+// Two workgroups of four wavefronts on a CU, or one of eight.  Of these estimates of the first launch's time, in us, with what its partials cost beside it, the least:
+// a workgroup on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront, on a chip that they do not fill less of
+// it; all of them together, spread evenly, and at the end a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip,
+// whole rounds; the longest alone; all rows at the memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.
+// Measured on 110 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 120 choices each, the estimates' choice was 2 .. 5 %
+// from the best on average, with eight wavefronts alone 4 .. 5 % more.  Eight are chosen for groups of more than 128 columns only: with fewer four were the better by 5 %
+// (to 64) and 1 % (to 128) on average; 256 requests behind three documents, 32 / 8 heads, take 423 us with eight and 520 with four.
+static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    constexpr double kOwnStart = 5.5, kOwnTile = 3.5, kTail = 0.25, kTailOwn = 0.4, kTailBoth = 0.135, kFewRounds = 2.2, kWholeRound = 1.1, kPartial = 0.0065, kBytesPerUs = 6.1e6;
+    constexpr double kAlone = 0.53, kBlocks = 1.16;                 // of a step's time: on a chip that is hardly filled; where more than one block of four tiles reads the rows
     struct Times { double start, step; };
-    constexpr Times kTimes[4] = {{7, 4.5}, {8, 2.7}, {9, 1.25}, {10, 1.15}};   // of a workgroup with 1, 2, 4, 8 column tiles
+    constexpr Times kTimes[4] = {{6, 3.8}, {7.7, 2.3}, {7.7, 1.2}, {20, 0.92}};   // of a workgroup with 1, 2, 4, 8 column tiles
     constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
-    static_assert(kRanges[10] == kSharedMost && kOwnRanges[5] == kSharedOwn, "their slots lie in LDS");
+    static_assert(kOwnRanges[5] == SharedGeometry<4>::own && kOwnRanges[5] == SharedGeometry<8>::own, "their slots lie in LDS");
     SharedPlan p = {};
     const int64_t G = Hq / Hkv, chunks = (G + 31) / 32, mean = n_groups > 1 ? (B + n_groups / 2) / n_groups : max_group, rows = (mean > 1 ? mean : 1) * G;
-    const int cols = shared_cols(rows), kind = __builtin_ctz(cols);
-    const int64_t step = 32 * (kSharedWaves / cols), wide = Hkv * ((rows + 32 * cols - 1) / (32 * cols));
-    const double own_tiles = (double)total_tokens / 32 * Hkv * chunks / kSharedWaves;
+    const int cols = shared_cols(rows, waves), kind = __builtin_ctz(cols);
+    const double at_once = 256 * (8 / waves);
+    const int64_t step = 32 * (waves / cols), wide = Hkv * ((rows + 32 * cols - 1) / (32 * cols));
+    const double own_tiles = (double)total_tokens / 32 * Hkv * chunks / waves;
     const double memory = ((double)prefix_total + total_tokens) * Hkv * (4 * kHeadDim) / kBytesPerUs;
-    auto own_wgs = [&](int32_t range) { return total_tokens == 0 ? 0 : (((int64_t)total_tokens / range + B) * Hkv * chunks + kSharedWaves - 1) / kSharedWaves; };
-    double best_us = HUGE_VAL;
+    auto own_wgs = [&](int32_t range) { return total_tokens == 0 ? 0 : (((int64_t)total_tokens / range + B) * Hkv * chunks + waves - 1) / waves; };
+    p.us = HUGE_VAL;
     for (const int32_t range : kRanges) {
-        const double one = kTimes[kind].start + kTimes[kind].step * (double)((range + step - 1) / step);
-        const double wgs = (ceil((double)prefix_total / range) + 0.5 * (n_groups - 1)) * wide, prefix_us = wgs * one;
+        if (range > waves * 512) break;                             // (its slots lie in LDS)
+        const double wgs = (ceil((double)prefix_total / range) + 0.5 * (n_groups - 1)) * wide;
+        const double steps = (double)((range + step - 1) / step) * (kind == 2 && rows > 128 ? kBlocks : 1);
         for (const int32_t own_range : kOwnRanges) {
-            const double own = (double)own_wgs(own_range), longest = total_tokens == 0 ? one : fmax(one, kOwnStart + kOwnTile * own_range / 32);
-            const double sum = prefix_us + own * kOwnStart + own_tiles * kOwnTile, n = wgs + own;
-            const double mine = kOwnStart + kOwnTile * own_range / 32;
-            const double ends = own == 0 || n <= kOneAfter * kCus ? kTail * longest : kind <= 1 ? kTail * mine : kTailBoth * (mine + one);
-            double us = fmax(fmax(sum / kCus + ends, longest), memory);
-            if (n <= kFewRounds * kCus) us = fmax(us, kWholeRound * ceil(n / kCus) * sum / n);
+            const double own = (double)own_wgs(own_range), n = wgs + own, full = kAlone + (1 - kAlone) * fmin(1, n / at_once);
+            const double one = kTimes[kind].start + kTimes[kind].step * steps * full, prefix_us = wgs * one;
+            const double mine = kOwnStart + kOwnTile * full * own_range / 32, longest = total_tokens == 0 ? one : fmax(one, mine);
+            const double sum = prefix_us + own * kOwnStart + own_tiles * kOwnTile * full;
+            const double ends = own == 0 || n <= kOneAfter * at_once ? kTail * longest : kind <= 1 ? kTailOwn * mine : kTailBoth * (mine + one);
+            double us = fmax(fmax(sum / at_once + ends, longest), memory);
+            if (n <= kFewRounds * at_once) us = fmax(us, kWholeRound * ceil(n / at_once) * sum / n);
             us += wgs * cols * kPartial;
-            if (us < best_us) {
-                best_us = us; p.range = range; p.own_range = own_range;
-                p.share = prefix_us / sum; p.last = one / (sum / kCus);
+            if (us < p.us) {
+                p.us = us; p.range = range; p.own_range = own_range;
+                p.share = prefix_us / sum; p.last = one / (sum / at_once);
             }
             if (total_tokens == 0) break;
         }
         if (range >= prefix_total) break;
     }
-    p.us = best_us;
+    p.waves = waves;
     p.kind = kind;
-    p.blocks = (max_group * G + 255) / 256;                         // (fewer than eight column tiles are one block)
+    p.blocks = (max_group * G + 32 * waves - 1) / (32 * waves);     // (fewer column tiles than wavefronts are one block)
     p.slots = (size_t)(prefix_total / p.range) + n_groups;
     p.units = (int64_t)p.slots * Hkv;
     p.own = own_wgs(p.own_range);
     p.own_slots = (size_t)(total_tokens / p.own_range + B);         // (of requests of any lengths)
     return p;
+}
+static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    const SharedPlan four = shared_plan_for(4, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
+    if (four.kind < 2) return four;
+    const SharedPlan eight = shared_plan_for(8, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
+    return eight.kind == 3 && eight.us < four.us ? eight : four;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
@@ -682,17 +706,17 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
 }
 
 // Which calls run in one launch: those with no more workgroups than CUs whose estimate is the less.  In one launch: a start and an end, then the longest
-// list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 290
+// list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 280
 // calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
-// 20 behind 300, 4 / 4 heads, 12.1 -> 8.4, of 300 behind 1000 13.2 -> 16.1*; 16 of 300 behind 30, 32 / 8, 17.3 -> 10.5, 16 of 20 behind 1000 16.0 -> 14.5, behind
-// 2000 17.3 -> 22.0*; 32 of 300 behind 300, 32 / 1, 21.2 -> 14.0.  To the better form the choice loses 0.3 % on average, 18 % at most.
+// 20 behind 300, 4 / 4 heads, 11.3 -> 8.7, of 300 behind 1000 11.9 -> 16.1*; 16 of 300 behind 30, 32 / 8, 15.0 -> 10.7, 16 of 20 behind 1000 14.9 -> 14.6, behind
+// 2000 16.0 -> 22.0*; 32 of 300 behind 300, 32 / 1, 17.5 -> 14.0.  To the better form the choice loses 0.2 % on average, 9 % at most.
 static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
     const int32_t forced = forced_decode_plan();
     if (forced != 0) return forced == 2;
     const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
     if (a.B * (int64_t)a.Hkv * chunks > 256) return false;
     const double bytes = ((double)a.B * a.max_prefix + a.total_tokens) * a.Hkv * chunks * (4 * kHeadDim);
-    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 3.1 + 0.8 * p.us + 1.8 * p.kind;
+    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 2 + 1.07 * p.us + 1.75 * p.kind;
     return whole < 0.95 * ranges;
 }
 
@@ -705,7 +729,7 @@ static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
 // 4705, 32 / 4, 48.6 against 53.1.  (Workgroups that take one piece of work after another by a counter: 416, and their loop costs others 4 % in the mean.)
 static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own) {
     SharedWork w = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks, 0, 0, 0};
-    const int32_t P = w.prefix >> 3, N = w.own >> 3, all = P + N, round = 32;
+    const int32_t P = w.prefix >> 3, N = w.own >> 3, all = P + N, round = 32 * (8 / p.waves);
     if (all <= kOneAfter * round) {
         w.first = w.mixed = all;
         w.first_prefix = P;
@@ -730,21 +754,23 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     const SharedPlan p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
     if (shared_whole(a, p)) {
         const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
-        if (a.B > (int32_t)(UINT32_MAX / (kSharedWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
+        if (a.B > (int32_t)(UINT32_MAX / (kWholeWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
             return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many requests or heads for one launch of a workgroup each");
-        hipLaunchKernelGGL(shared_whole_kernel, dim3(a.B, a.Hkv, (unsigned)chunks), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e);
+        hipLaunchKernelGGL(shared_whole_kernel, dim3(a.B, a.Hkv, (unsigned)chunks), dim3(kWholeWaves * 64), 0, stream, a, a.softmax_scale * kLog2e);
         return check_launch("shared_whole_kernel");
     }
     const int32_t pairs = a.B * a.Hq;
     const int64_t prefix = (p.units + 7) / 8 * 8 * p.blocks, own = (p.own + 7) / 8 * 8;
-    if (prefix + own > (int64_t)(UINT32_MAX / (kSharedWaves * 64)) || p.units > INT32_MAX / 2)
+    if (prefix + own > (int64_t)(UINT32_MAX / (p.waves * 64)) || p.units > INT32_MAX / 2)
         return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
     float* const acc = (float*)workspace;
     const SharedParts parts = {acc, acc + p.slots * a.max_group * a.Hq * kHeadDim, p.range};
     float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
     const SharedParts mine = {own_acc, own_acc + p.own_slots * a.Hq * kHeadDim, p.own_range};
     const SharedWork work = shared_order(p, prefix, own);
-    hipLaunchKernelGGL(shared_partial_kernel, dim3((unsigned)(prefix + own)), dim3(kSharedWaves * 64), 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
+    const dim3 grid((unsigned)(prefix + own)), block(p.waves * 64);
+    if (p.waves == 8) hipLaunchKernelGGL(shared_partial_kernel<8>, grid, block, 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
+    else hipLaunchKernelGGL(shared_partial_kernel<4>, grid, block, 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
     const esp_status st = check_launch("shared_partial_kernel");
     if (st != ESP_OK) return st;
     const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair

@@ -353,6 +353,29 @@ def test_decode_behind_shared_prefixes(cuda, form, name, groups, prefixes, lens,
     assert torch.equal(O, O2) and torch.equal(LSE, L2)
 
 
+@pytest.mark.parametrize("groups,prefixes,lens,Hq,Hkv", [([64], [30000], [7] * 64, 32, 8), ([60, 1, 17, 90, 12], [30000, 300, 2100, 15000, 900], [7, 0, 40] * 60, 16, 4)],
+                         ids=["one", "ragged"])
+@pytest.mark.parametrize("far", [None, "prefix_slots", "slot_idx"], ids=["alike", "prefix", "own"])
+def test_shared_long_prefixes_of_many_columns(cuda, groups, prefixes, lens, Hq, Hkv, far):
+    """What runs by eight wavefronts that have a CU alone, beside it groups of fewer columns; scores of one side far above the other's; a NaN that stays in its head."""
+    call, both = shared_inputs(cuda, groups, prefixes, lens, Hq, Hkv, 31)
+    if far:
+        call["k_pool"][call[far].long()] *= 40
+    Or, Lr = shared_reference(call, both, cuda)
+    ws = shared_workspace(call, cuda)
+    O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=ws)
+    check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), str(far))
+    O2, L2 = esp.esp_partial_attn_decode_shared(**call)
+    assert torch.equal(O, O2) and torch.equal(LSE, L2)
+    if not far:
+        call["k_pool"][call["prefix_slots"][12345].long(), 1] = float("nan")
+        O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=ws)
+        h, n = slice(Hq // Hkv, 2 * (Hq // Hkv)), groups[0]
+        assert torch.isnan(LSE[:n, h]).all() and torch.isnan(O[:n, h]).all()
+        O[:n, h], LSE[:n, h] = O2[:n, h], L2[:n, h]
+        assert torch.equal(O, O2) and torch.equal(LSE, L2)
+
+
 def test_shared_bounds_larger_than_what_is_there(cuda, form):
     call, both = shared_inputs(cuda, [3, 2], [200, 90], [5, 0, 7, 9, 1], 8, 2, 5)
     Or, Lr = shared_reference(call, both, cuda)
