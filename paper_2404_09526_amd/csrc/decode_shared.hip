@@ -642,8 +642,10 @@ constexpr double kOneAfter = 1.6;
 // it; all of them together, spread evenly, and at the end a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip,
 // whole rounds; the longest alone; all rows at the memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.
 // Measured on 110 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 120 choices each, the estimates' choice was 2 .. 5 %
-// from the best on average, with eight wavefronts alone 4 .. 5 % more.  Eight are chosen for groups of more than 128 columns only: with fewer four were the better by 5 %
-// (to 64) and 1 % (to 128) on average; 256 requests behind three documents, 32 / 8 heads, take 423 us with eight and 520 with four.
+// from the best on average, with eight wavefronts alone 4 .. 5 % more.  At their best four were the better by 5 % (groups of up
+// to 64 columns) and 2 % (more) on average, each way by up to 20 % for some: 256 requests behind three documents, 32 / 8 heads, take 423 us with eight and 520 with four, 46 behind
+// some 1000 tokens each in five groups, 32 / 32, 51 and 42.  Eight are taken for up to 128 columns where they are 6 % the less, which is the better choice on those batches by
+// 0.7 % (where they are the less at all: by 1.7 % the worse).
 static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
     constexpr double kOwnStart = 5.5, kOwnTile = 3.5, kTail = 0.25, kTailOwn = 0.4, kTailBoth = 0.135, kFewRounds = 2.2, kWholeRound = 1.1, kPartial = 0.0065, kBytesPerUs = 6.1e6;
     constexpr double kAlone = 0.53, kBlocks = 1.16;                 // of a step's time: on a chip that is hardly filled; where more than one block of four tiles reads the rows
@@ -692,9 +694,8 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
 }
 static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
     const SharedPlan four = shared_plan_for(4, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
-    if (four.kind < 2) return four;
     const SharedPlan eight = shared_plan_for(8, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
-    return eight.kind == 3 && eight.us < four.us ? eight : four;
+    return eight.us * (eight.kind == 3 ? 1 : 1.06) < four.us ? eight : four;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
