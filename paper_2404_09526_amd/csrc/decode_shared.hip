@@ -777,7 +777,10 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_
     const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair
 #define ESP_COMBINE_LAUNCH(GROUPS)                                                                                                          \
     hipLaunchKernelGGL((shared_combine_kernel<GROUPS>), row_grid(((int64_t)pairs + 8 / GROUPS - 1) / (8 / GROUPS)), dim3(256), 0, stream, a, pairs, parts, mine)
-    if (most <= 64) ESP_COMBINE_LAUNCH(2);
+    // A wavefront to a pair, which takes eight partials at a time, or a workgroup, which takes 32 and joins them through LDS: this where there are so many, or pairs
+    // so few that a wavefront's rounds are all that the launch is.  On 210 batches that is 2 % less than a wavefront up to 64 partials (one request behind 14159
+    // tokens beside three alone, 24 / 3 heads, 18.9 -> 15.2 us).
+    if (most <= 8 || (most <= 64 && pairs > 2048)) ESP_COMBINE_LAUNCH(2);
     else ESP_COMBINE_LAUNCH(8);
 #undef ESP_COMBINE_LAUNCH
     return check_launch("shared_combine_kernel");
