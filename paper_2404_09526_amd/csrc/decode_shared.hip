@@ -8,8 +8,8 @@
 // ranges side by side, and what bounds the one is left over by the other (shared_order).  A second launch combines the partials of both kinds.
 // Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes of many columns, which
 // read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
-// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 51 us (207 MB); 16 behind 65536, 32 / 32, 222 (1.24 GB, 5.6 TB/s); 256 in three groups behind 65549,
-// 40000 and 20011, 32 / 8, 420 (1.59 GB and 193 GFLOP); four short requests 7.5.
+// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 51 us (207 MB); 16 behind 65536, 32 / 32, 220 (1.24 GB, 5.6 TB/s); 256 in three groups behind 65549,
+// 40000 and 20011, 32 / 8, 410 (1.59 GB and 193 GFLOP); four short requests 7.5.
 #include <math.h>
 
 #include "column_tile.h"
@@ -709,8 +709,8 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
 // Which calls run in one launch: those with no more workgroups than CUs whose estimate is the less.  In one launch: a start and an end, then the longest
 // list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 280
 // calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
-// 20 behind 300, 4 / 4 heads, 11.3 -> 8.7, of 300 behind 1000 11.9 -> 16.1*; 16 of 300 behind 30, 32 / 8, 15.0 -> 10.7, 16 of 20 behind 1000 14.9 -> 14.6, behind
-// 2000 16.0 -> 22.0*; 32 of 300 behind 300, 32 / 1, 17.5 -> 14.0.  To the better form the choice loses 0.2 % on average, 9 % at most.
+// 20 behind 300, 4 / 4 heads, 11.3 -> 8.5, of 300 behind 1000 11.6 -> 16.1*; 16 of 300 behind 30, 32 / 8, 14.8 -> 10.7, 16 of 20 behind 1000 15.6 -> 14.3, behind
+// 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.2 % on average, 26 % at most.
 static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
     const int32_t forced = forced_decode_plan();
     if (forced != 0) return forced == 2;
