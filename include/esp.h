@@ -362,6 +362,7 @@ esp_status esp_partial_attn_prefill_pool_direct(
  *   Everything else as in esp_partial_attn_decode (max_len: of the requests' own
  *   lists).  B = 0 writes nothing.  n_groups = 0 needs prefix_total = 0: the group arrays may
  *   then be NULL.
+ *   q, the pools and O lie on 16 bytes (ESP_ERR_INVALID_ARG).
  *   workspace: at least esp_decode_shared_workspace_bytes(...) bytes, 256-byte
  *   aligned; contents need not be preserved.  0 from there: the call would be refused.
  * With esp_debug_set_validate the two lists and three offset arrays are checked as

@@ -388,6 +388,8 @@ esp_status esp_partial_attn_decode_shared(const void* q, const void* k_pool, con
     if (n_groups > 0 && (!prefix_offsets || !group_offsets)) return fail(ESP_ERR_INVALID_ARG, "decode (shared): null prefix_offsets/group_offsets");
     if (prefix_total > 0 && (!k_pool || !v_pool || !prefix_slots || num_slots == 0))
         return fail(ESP_ERR_INVALID_ARG, "decode (shared): null pool/prefix_slots");
+    for (const void* p : {q, k_pool, v_pool, (const void*)O})
+        if ((uintptr_t)p & 15) return fail(ESP_ERR_INVALID_ARG, "decode (shared): a pointer is not 16-byte aligned");
     const size_t need = decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv);
     if (!workspace || workspace_bytes < need)
         return fail(ESP_ERR_WORKSPACE, "decode (shared): workspace needs %zu bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);

@@ -384,6 +384,28 @@ def test_shared_bounds_larger_than_what_is_there(cuda, form):
     check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), "bounds")
 
 
+def test_shared_requests_past_the_stated_group_are_left_without_the_prefix(cuda, form):
+    call, both = shared_inputs(cuda, [3, 40], [200, 90], [5, 0, 7] + [3] * 40, 8, 2, 41)
+    for b in [2] + list(range(5, 43)):
+        both[b] = both[b][200 if b < 3 else 90:]
+    call["max_group"] = 2
+    Or, Lr = shared_reference(call, both, cuda)
+    O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=shared_workspace(call, cuda))
+    check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), "bounds")
+
+
+def test_shared_rows_named_twice_count_twice(cuda, form):
+    """In a list, in a prefix and in a request's own list, in the prefixes of two groups."""
+    call, both = shared_inputs(cuda, [3, 40], [200, 90], [5, 0, 7] + [3] * 40, 8, 2, 42)
+    prefix, own = call["prefix_slots"], call["slot_idx"]
+    prefix[7], prefix[60:80], prefix[200:260], own[2:5], own[6] = prefix[3], prefix[150], prefix[:60], prefix[150:153], own[5]
+    p, s, po, so = prefix.cpu().numpy(), own.cpu().numpy(), offsets([200, 90]), offsets([5, 0, 7] + [3] * 40)
+    both = [np.concatenate([p[po[int(b >= 3)]:po[int(b >= 3) + 1]], s[so[b]:so[b + 1]]]) for b in range(43)]
+    Or, Lr = shared_reference(call, both, cuda)
+    O, LSE = esp.esp_partial_attn_decode_shared(**call, workspace=shared_workspace(call, cuda))
+    check_o_lse(f64(O).reshape(-1, 128), LSE.cpu().numpy().reshape(-1), Or.reshape(-1, 128), Lr.reshape(-1), "twice")
+
+
 def test_shared_without_groups_is_plain_decode(cuda, form):
     call, both = shared_inputs(cuda, [3], [0], [50, 0, 7], 8, 2, 6)
     Or, Lr = shared_reference(call, both, cuda)

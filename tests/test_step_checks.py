@@ -70,7 +70,7 @@ def test_decode_behind_shared_prefixes(lib):
     assert call(D=64) == lib.ESP_ERR_UNSUPPORTED
     for kw in (dict(B=-1), dict(n_groups=-1), dict(P_total=-1), dict(max_prefix=-1), dict(max_group=-1), dict(max_prefix=101), dict(max_group=4), dict(n_groups=0), dict(max_len=11),
                dict(Hq=6, Hkv=4), dict(q=nul), dict(kp=nul), dict(S=0), dict(ps=nul), dict(po=nul), dict(go=nul), dict(idx=nul), dict(off=nul), dict(O=nul), dict(LSE=nul),
-               dict(scale=float("nan")), dict(scale=-1.0)):
+               dict(scale=float("nan")), dict(scale=-1.0), dict(q=P(264)), dict(kp=P(258)), dict(O=P(260))):
         assert call(**kw) == bad, kw
     for kw in (dict(ws=nul), dict(ws_bytes=need - 1), dict(ws=P(264))):
         assert call(**kw) == lib.ESP_ERR_WORKSPACE, kw
