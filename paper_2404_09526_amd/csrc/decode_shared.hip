@@ -185,7 +185,7 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
 // and K of step j + 1.
 // A team of one wavefront shares nothing: it waits for its own rows only (sweep_tiles).
 struct PrefixPart { RequestRange at; int32_t b0, seg, n_all, kvh; };  // a range of group at.b's prefix: its keys, the group's first request and packed rows
-template <int WAVES, int COLS>
+template <int WAVES, int COLS, bool ONCE>
 __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, const PrefixPart& part, uint32_t cb, unsigned char* smem,
                                               int wave, int lane) {
     constexpr int TEAMS = WAVES / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
@@ -230,9 +230,10 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
         // A wavefront's rows of a tile are the same for K and V: slots are looked up a group ahead, and a row's place is kept from K's group to V's.
         uint32_t slot[MOVES];
         uint64_t place[MOVES];
-        // (Up to four column tiles are all that there are, and the rows pass once.  Of eight there may be more workgroups on the same rows.)
+        // ONCE: these columns are all that the group has, and the rows pass once; otherwise other workgroups find them in the L2.  (4 requests behind 100 thousand tokens are
+        // 8 % faster past the caches, 100 behind 65536 8 % slower.)
         auto fetch_row = [](uint32_t to, const char* from) {
-            if constexpr (COLS < 8) load_to_lds_b128_at_nt(to, from);
+            if constexpr (ONCE) load_to_lds_b128_at_nt(to, from);
             else load_to_lds_b128_at(to, from);
         };
         auto look_up = [&](int i) {
@@ -453,11 +454,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void shared_partial_kernel(SharedArg
     part.n_all = min(min(b1, a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
     part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
     if (part.seg <= 0 || part.n_all <= 0) return;
-    switch (shared_cols(part.n_all, WAVES)) {
-        case 1: shared_prefix<WAVES, 1>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        case 2: shared_prefix<WAVES, 2>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        case 4: shared_prefix<WAVES, 4>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
-        default: shared_prefix<WAVES, WAVES>(a, scale_log2, parts, part, cb, smem, wave, lane);
+    if (part.n_all > 32 * WAVES) shared_prefix<WAVES, WAVES, false>(a, scale_log2, parts, part, cb, smem, wave, lane);
+    else switch (shared_cols(part.n_all, WAVES)) {
+        case 1: shared_prefix<WAVES, 1, true>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 2: shared_prefix<WAVES, 2, true>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        case 4: shared_prefix<WAVES, 4, true>(a, scale_log2, parts, part, cb, smem, wave, lane); break;
+        default: shared_prefix<WAVES, WAVES, false>(a, scale_log2, parts, part, cb, smem, wave, lane);   // (eight: 2 % from the caches for less code)
     }
 }
 
@@ -641,16 +643,15 @@ constexpr double kOneAfter = 1.6;
 // a workgroup on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront, on a chip that they do not fill less of
 // it; all of them together, spread evenly, and at the end a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip,
 // whole rounds; the longest alone; all rows at the memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.
-// Measured on 110 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 120 choices each, the estimates' choice was 2 .. 5 %
-// from the best on average, with eight wavefronts alone 4 .. 5 % more.  At their best four were the better by 5 % (groups of up
-// to 64 columns) and 2 % (more) on average, each way by up to 20 % for some: 256 requests behind three documents, 32 / 8 heads, take 423 us with eight and 520 with four, 46 behind
-// some 1000 tokens each in five groups, 32 / 32, 51 and 42.  Eight are taken for up to 128 columns where they are 6 % the less, which is the better choice on those batches by
-// 0.7 % (where they are the less at all: by 1.7 % the worse).
+// Measured on 127 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 120 choices each, the estimates' choice was 5 %
+// from the best on average.  Four wavefronts at their best were the better by 5 % on average; eight were it for few and long ranges and for much work of more than 128 columns
+// and nothing else (64 requests behind 130000 tokens, 32 / 8 heads, 207 us with eight, 222 with four; 256 behind three documents and their own rows 438 and 413).
+// So eight are taken where their estimate is 6 %, with more than 128 columns 8 %, the less (where it is less at all: 2 .. 3 % more time on average).
 static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    constexpr double kOwnStart = 5.5, kOwnTile = 3.5, kTail = 0.25, kTailOwn = 0.4, kTailBoth = 0.135, kFewRounds = 2.2, kWholeRound = 1.1, kPartial = 0.0065, kBytesPerUs = 6.1e6;
-    constexpr double kAlone = 0.53, kBlocks = 1.16;                 // of a step's time: on a chip that is hardly filled; where more than one block of four tiles reads the rows
+    constexpr double kOwnStart = 5.5, kOwnTile = 3.6, kTail = 0.15, kTailOwn = 0.375, kTailBoth = 0.23, kFewRounds = 2.2, kWholeRound = 1.1, kPartial = 0.0054, kBytesPerUs = 5.95e6;
+    constexpr double kAlone = 0.41, kBlocks = 0.855;                // of a step's time: on a chip that is hardly filled; where blocks of four tiles find rows in the L2
     struct Times { double start, step; };
-    constexpr Times kTimes[4] = {{6, 3.8}, {7.7, 2.3}, {7.7, 1.2}, {20, 0.92}};   // of a workgroup with 1, 2, 4, 8 column tiles
+    constexpr Times kTimes[4] = {{5.4, 4}, {12.2, 1.35}, {8.2, 1.5}, {15.8, 1.03}};   // of a workgroup with 1, 2, 4, 8 column tiles
     constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
     static_assert(kOwnRanges[5] == SharedGeometry<4>::own && kOwnRanges[5] == SharedGeometry<8>::own, "their slots lie in LDS");
     SharedPlan p = {};
@@ -695,7 +696,7 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
 static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
     const SharedPlan four = shared_plan_for(4, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
     const SharedPlan eight = shared_plan_for(8, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
-    return eight.us * (eight.kind == 3 ? 1 : 1.06) < four.us ? eight : four;
+    return eight.us * (eight.kind == 3 ? 1.08 : 1.06) < four.us ? eight : four;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
@@ -710,15 +711,15 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
 // list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 280
 // calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
 // 20 behind 300, 4 / 4 heads, 11.3 -> 8.5, of 300 behind 1000 11.6 -> 16.1*; 16 of 300 behind 30, 32 / 8, 14.8 -> 10.7, 16 of 20 behind 1000 15.6 -> 14.3, behind
-// 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.2 % on average, 26 % at most.
+// 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.3 % on average, 26 % at most.
 static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
     const int32_t forced = forced_decode_plan();
     if (forced != 0) return forced == 2;
     const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
     if (a.B * (int64_t)a.Hkv * chunks > 256) return false;
     const double bytes = ((double)a.B * a.max_prefix + a.total_tokens) * a.Hkv * chunks * (4 * kHeadDim);
-    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 2 + 1.07 * p.us + 1.75 * p.kind;
-    return whole < 0.95 * ranges;
+    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 4.6 + 0.82 * p.us + 1.4 * p.kind;
+    return whole < 0.97 * ranges;
 }
 
 // The order of the first launch.  Workgroups start in the order of their numbers as others end (on each XCD, and there on one shader engine after the other:

@@ -353,11 +353,13 @@ def test_decode_behind_shared_prefixes(cuda, form, name, groups, prefixes, lens,
     assert torch.equal(O, O2) and torch.equal(LSE, L2)
 
 
-@pytest.mark.parametrize("groups,prefixes,lens,Hq,Hkv", [([64], [30000], [7] * 64, 32, 8), ([60, 1, 17, 90, 12], [30000, 300, 2100, 15000, 900], [7, 0, 40] * 60, 16, 4)],
-                         ids=["one", "ragged"])
+@pytest.mark.parametrize("groups,prefixes,lens,Hq,Hkv", [([136], [20000], [7] * 136, 16, 16), ([70, 2, 9, 15, 33, 60], [16000, 320, 1120, 1600, 800, 16000], [7, 0, 40] * 63, 8, 2),
+                                                         ([64], [30000], [7] * 64, 32, 8)],
+                         ids=["one", "ragged", "blocks"])
 @pytest.mark.parametrize("far", [None, "prefix_slots", "slot_idx"], ids=["alike", "prefix", "own"])
 def test_shared_long_prefixes_of_many_columns(cuda, groups, prefixes, lens, Hq, Hkv, far):
-    """What runs by eight wavefronts that have a CU alone, beside it groups of fewer columns; scores of one side far above the other's; a NaN that stays in its head."""
+    """The first two by eight wavefronts that have a CU alone (groups of all numbers of columns), the third by four in blocks of columns; scores of one side far above the
+    other's; a NaN that stays in its head."""
     call, both = shared_inputs(cuda, groups, prefixes, lens, Hq, Hkv, 31)
     if far:
         call["k_pool"][call[far].long()] *= 40
