@@ -6,10 +6,10 @@
 // against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row).  With few columns the prefix is bound by the
 // memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
 // ranges side by side, and what bounds the one is left over by the other (shared_order).  A second launch combines the partials of both kinds.
-// Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes of many columns, which
-// read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
-// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 51 us (207 MB); 16 behind 65536, 32 / 32, 220 (1.24 GB, 5.6 TB/s); 256 in three groups behind 65549,
-// 40000 and 20011, 32 / 8, 410 (1.59 GB and 193 GFLOP); four short requests 7.5.
+// Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes of many columns and little
+// else, which read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
+// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 52 us (207 MB); 16 behind 65536, 32 / 32, 219 (1.24 GB, 5.7 TB/s); 256 in three groups behind 65549,
+// 40000 and 20011, 32 / 8, 419 (1.59 GB and 193 GFLOP); four short requests 7.5.
 #include <math.h>
 
 #include "column_tile.h"
@@ -726,9 +726,10 @@ static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
 // one that is full holds up what comes behind).  What ends last should be short, and the prefix's workgroups are the long ones: so of those that start together as
 // many are the prefix's as its share of the time, the rest follow evenly, and own rows alone fill the time that the last of the prefix take, and half as much
 // again (their last ranges are short).  A prefix with few columns is bound by the memory as own rows are, nothing is gained side by side, and it comes first.
-// Evenly mixed -> so: 96 + 100 + 60 requests behind 66, 40 and 20 thousand tokens, 32 / 8 heads, 442 -> 418 us; 1 + 110 + 12 behind 12452, 947 and 28, 32 / 8, 71 -> 56;
-// 16 behind 65536, 32 / 32, 243 -> 234.  Up to 1.6 rounds of the chip it matters which ones the second gets, and evenly mixed is the better: 25 + 38 behind 16464 and
-// 4705, 32 / 4, 48.6 against 53.1.  (Workgroups that take one piece of work after another by a counter: 416, and their loop costs others 4 % in the mean.)
+// Over 210 batches an even mixture takes 2.5 % more time, up to 63 % for one: 16 requests behind 65536 tokens, 32 / 32 heads, 245 us against 223; with eight wavefronts 1 + 110 + 12
+// behind 12452, 947 and 28, 32 / 8, 71 against 56, and 96 + 100 + 60 behind 66, 40 and 20 thousand 442 against 418 (prefix first: 468 with four).  Up to 1.6 rounds of the chip it
+// matters which ones the second gets, and evenly mixed is the better: 25 + 38 behind 16464 and 4705, 32 / 4, 48.6 against 53.1.  (Workgroups that take one piece of work after
+// another by a counter: 416, and their loop costs others 4 % in the mean.)
 static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own) {
     SharedWork w = {(int32_t)prefix, (int32_t)own, (int32_t)p.units, (int32_t)p.blocks, 0, 0, 0};
     const int32_t P = w.prefix >> 3, N = w.own >> 3, all = P + N, round = 32 * (8 / p.waves);
