@@ -699,12 +699,12 @@ static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total,
     return eight.us * (eight.kind == 3 ? 1.08 : 1.06) < four.us ? eight : four;
 }
 static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
+static size_t partials_bytes(const SharedPlan& p, int32_t max_group, int32_t Hq) { return partials_bytes(p.slots, (int64_t)max_group * Hq) + partials_bytes(p.own_slots, Hq); }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
                                      int32_t Hq, int32_t Hkv) {
     (void)max_prefix;
     if (prefix_total == 0 || max_group == 0) return decode_workspace_bytes(B, total_tokens, Hq, Hkv);
-    const SharedPlan p = shared_plan(B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
-    return partials_bytes(p.slots, (int64_t)max_group * Hq) + partials_bytes(p.own_slots, Hq);
+    return partials_bytes(shared_plan(B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv), max_group, Hq);
 }
 
 // Which calls run in one launch: those with no more workgroups than CUs whose estimate is the less.  In one launch: a start and an end, then the longest
@@ -749,12 +749,16 @@ static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own)
     return w;
 }
 
-esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_t stream) {
-    if (a.prefix_total == 0 || a.max_group == 0)
-        return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
-                             workspace, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream);
+esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    const bool alone = a.prefix_total == 0 || a.max_group == 0;     // no prefix: the plain decode
     if ((int64_t)a.B * a.Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode (shared): too many rows for one launch");
-    const SharedPlan p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
+    SharedPlan p = {};
+    if (!alone) p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
+    const size_t need = alone ? decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv) : partials_bytes(p, a.max_group, a.Hq);
+    if (workspace_bytes < need) return fail(ESP_ERR_WORKSPACE, "decode (shared): workspace needs %zu bytes, got %zu", need, workspace_bytes);
+    if (alone)
+        return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
+                             workspace, need, stream);
     if (shared_whole(a, p)) {
         const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
         if (a.B > (int32_t)(UINT32_MAX / (kWholeWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)

@@ -100,7 +100,7 @@ struct SharedArgs {
 };
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
                                      int32_t Hq, int32_t Hkv);
-esp_status launch_decode_shared(const SharedArgs& a, void* workspace, hipStream_t stream);
+esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 // The request that holds token t, the last b with seq_offsets[b] <= t, and where it ends; found by a wavefront 64 candidates at a
 // time (a binary search is six dependent loads, about 3 us, at 64 requests; this is one).
