@@ -21,7 +21,7 @@ constexpr int kSharedTile = kColKBytes + kColVBytes;
 // A workgroup of the first launch has four wavefronts, two of them share a CU, or eight, which have it alone.
 template <int WAVES>
 struct SharedGeometry {
-    static constexpr int half = WAVES * (kSharedTile / 2), most = WAVES * 512;   // of the tiles' LDS; keys of a prefix range: its slots lie in LDS
+    static constexpr int half = WAVES * (kSharedTile / 2), most = 4096;   // of the tiles' LDS; keys of a prefix range: its slots lie in LDS
     static constexpr int own = 512;                                 // keys of an own range, a wavefront's: its slots too
     static constexpr int lds = 2 * half + most * 4;
     // tiles that wavefronts have for themselves lie before the lists; the blocks that rows are stored from, which are larger, may lie on them: they come last
@@ -653,7 +653,7 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
     struct Times { double start, step; };
     constexpr Times kTimes[4] = {{5.4, 4}, {12.2, 1.35}, {8.2, 1.5}, {15.8, 1.03}};   // of a workgroup with 1, 2, 4, 8 column tiles
     constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
-    static_assert(kOwnRanges[5] == SharedGeometry<4>::own && kOwnRanges[5] == SharedGeometry<8>::own, "their slots lie in LDS");
+    static_assert(kRanges[10] == SharedGeometry<4>::most && kRanges[10] == SharedGeometry<8>::most && kOwnRanges[5] == SharedGeometry<4>::own, "their slots lie in LDS");
     SharedPlan p = {};
     const int64_t G = Hq / Hkv, chunks = (G + 31) / 32, mean = n_groups > 1 ? (B + n_groups / 2) / n_groups : max_group, rows = (mean > 1 ? mean : 1) * G;
     const int cols = shared_cols(rows, waves), kind = __builtin_ctz(cols);
@@ -664,7 +664,6 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
     auto own_wgs = [&](int32_t range) { return total_tokens == 0 ? 0 : (((int64_t)total_tokens / range + B) * Hkv * chunks + waves - 1) / waves; };
     p.us = HUGE_VAL;
     for (const int32_t range : kRanges) {
-        if (range > waves * 512) break;                             // (its slots lie in LDS)
         const double wgs = (ceil((double)prefix_total / range) + 0.5 * (n_groups - 1)) * wide;
         const double steps = (double)((range + step - 1) / step) * (kind == 2 && rows > 128 ? kBlocks : 1);
         for (const int32_t own_range : kOwnRanges) {
