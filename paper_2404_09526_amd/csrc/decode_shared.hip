@@ -643,15 +643,15 @@ constexpr double kOneAfter = 1.6;
 // a workgroup on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront, on a chip that they do not fill less of
 // it; all of them together, spread evenly, and at the end a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip,
 // whole rounds; the longest alone; all rows at the memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.
-// Measured on 127 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 120 choices each, the estimates' choice was 5 %
-// from the best on average.  Four wavefronts at their best were the better by 5 % on average; eight were it for few and long ranges and for much work of more than 128 columns
-// and nothing else (64 requests behind 130000 tokens, 32 / 8 heads, 207 us with eight, 222 with four; 256 behind three documents and their own rows 438 and 413).
-// So eight are taken where their estimate is 6 %, with more than 128 columns 8 %, the less (where it is less at all: 2 .. 3 % more time on average).
+// Measured on 247 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 130 choices each, the estimates' choice was 5.5 %
+// from the best on average.  Four wavefronts at their best were the better by 6 % on average; eight were it for few long ranges (3 + 18 + 2 requests behind 47634, 102 and 3466 tokens,
+// 32 / 4 heads, 30 us with eight, 44 with four; 16 behind 130000, 32 / 8, 115 and 127) and by 2 % for much work of more than 128 columns and nothing else.  So
+// eight are taken where their estimate is 6 %, with more than 128 columns 8 %, the less (where it is less at all: 2 .. 3 % more time on average).
 static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    constexpr double kOwnStart = 5.5, kOwnTile = 3.6, kTail = 0.15, kTailOwn = 0.375, kTailBoth = 0.23, kFewRounds = 2.2, kWholeRound = 1.1, kPartial = 0.0054, kBytesPerUs = 5.95e6;
-    constexpr double kAlone = 0.41, kBlocks = 0.855;                // of a step's time: on a chip that is hardly filled; where blocks of four tiles find rows in the L2
+    constexpr double kOwnStart = 5.5, kOwnTile = 3.6, kTail = 0.15, kTailOwn = 0.44, kTailBoth = 0.23, kFewRounds = 3, kWholeRound = 1.1, kPartial = 0.0055, kBytesPerUs = 5.95e6;
+    constexpr double kAlone = 0.43, kBlocks = 0.865;                // of a step's time: on a chip that is hardly filled; where blocks of four tiles find rows in the L2
     struct Times { double start, step; };
-    constexpr Times kTimes[4] = {{5.4, 4}, {12.2, 1.35}, {8.2, 1.5}, {15.8, 1.03}};   // of a workgroup with 1, 2, 4, 8 column tiles
+    constexpr Times kTimes[4] = {{5.6, 4.15}, {12.1, 1.57}, {8.3, 1.48}, {15.5, 1.04}};   // of a workgroup with 1, 2, 4, 8 column tiles
     constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
     static_assert(kRanges[10] == SharedGeometry<4>::most && kRanges[10] == SharedGeometry<8>::most && kOwnRanges[5] == SharedGeometry<4>::own, "their slots lie in LDS");
     SharedPlan p = {};
