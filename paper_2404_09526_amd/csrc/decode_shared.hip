@@ -6,10 +6,10 @@
 // against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row).  With few columns the prefix is bound by the
 // memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
 // ranges side by side, and what bounds the one is left over by the other (shared_order).  A second launch combines the partials of both kinds.
-// Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes of many columns and little
+// Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes and little
 // else, which read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
-// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 52 us (207 MB); 16 behind 65536, 32 / 32, 219 (1.24 GB, 5.7 TB/s); 256 in three groups behind 65549,
-// 40000 and 20011, 32 / 8, 419 (1.59 GB and 193 GFLOP); four short requests 7.5.
+// Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 52 us (207 MB); 16 behind 65536, 32 / 32, 213 (1.24 GB, 5.8 TB/s); 256 in three groups behind 65549,
+// 40000 and 20011, 32 / 8, 416 (1.59 GB and 193 GFLOP); four short requests 7.5.
 #include <math.h>
 
 #include "column_tile.h"
