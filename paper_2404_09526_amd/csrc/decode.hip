@@ -553,7 +553,7 @@ esp_status launch_decode(const void* q, const void* k_pool, const void* v_pool, 
                          hipStream_t stream, const MergeArgs* peers, int32_t n_peers) {
     if (decode_whole(B, total_tokens, max_len, Hq, Hkv))
         return launch_decode_whole(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, Hq, Hkv, decode_burst_layout(Hq, Hkv),
-                                   softmax_scale * kLog2e, O, LSE, peers, n_peers, stream);
+                                   decode_burst_layout(Hq, Hkv) ? softmax_scale * kLog2e : score_factor(softmax_scale), O, LSE, peers, n_peers, stream);
     if ((int64_t)B * Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode: too many rows for one launch");
     const int32_t pairs = B * Hq;
     DecodeGeom g = decode_geom(B, total_tokens, Hq, Hkv, workspace_bytes);
@@ -564,7 +564,7 @@ esp_status launch_decode(const void* q, const void* k_pool, const void* v_pool, 
     const int G = Hq / Hkv;
     if (total_tokens > 0 && g.nhb_wg == 0) {
         esp_status st = launch_decode_gq(q, k_pool, v_pool, slot_idx, seq_offsets, B, total_tokens, g.range, parts, g.nwg, Hq, Hkv,
-                                         softmax_scale * kLog2e, part_acc, part_ml, stream);
+                                         score_factor(softmax_scale), part_acc, part_ml, stream);
         if (st != ESP_OK) return st;
     } else if (total_tokens > 0) {
         dim3 grid(parts > 0 ? B * parts : parts < 0 ? g.nwg + B : g.nwg, g.ygroups), block(kDecWaves * 64);

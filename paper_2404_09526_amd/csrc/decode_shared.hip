@@ -762,7 +762,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t wor
         const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
         if (a.B > (int32_t)(UINT32_MAX / (kWholeWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
             return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many requests or heads for one launch of a workgroup each");
-        hipLaunchKernelGGL(shared_whole_kernel, dim3(a.B, a.Hkv, (unsigned)chunks), dim3(kWholeWaves * 64), 0, stream, a, a.softmax_scale * kLog2e);
+        hipLaunchKernelGGL(shared_whole_kernel, dim3(a.B, a.Hkv, (unsigned)chunks), dim3(kWholeWaves * 64), 0, stream, a, score_factor(a.softmax_scale));
         return check_launch("shared_whole_kernel");
     }
     const int32_t pairs = a.B * a.Hq;
@@ -775,8 +775,8 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t wor
     const SharedParts mine = {own_acc, own_acc + p.own_slots * a.Hq * kHeadDim, p.own_range};
     const SharedWork work = shared_order(p, prefix, own);
     const dim3 grid((unsigned)(prefix + own)), block(p.waves * 64);
-    if (p.waves == 8) hipLaunchKernelGGL(shared_partial_kernel<8>, grid, block, 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
-    else hipLaunchKernelGGL(shared_partial_kernel<4>, grid, block, 0, stream, a, a.softmax_scale * kLog2e, parts, mine, work);
+    if (p.waves == 8) hipLaunchKernelGGL(shared_partial_kernel<8>, grid, block, 0, stream, a, score_factor(a.softmax_scale), parts, mine, work);
+    else hipLaunchKernelGGL(shared_partial_kernel<4>, grid, block, 0, stream, a, score_factor(a.softmax_scale), parts, mine, work);
     const esp_status st = check_launch("shared_partial_kernel");
     if (st != ESP_OK) return st;
     const int64_t most = (int64_t)a.max_prefix / p.range + a.max_len / p.own_range + 3;   // partials of a pair

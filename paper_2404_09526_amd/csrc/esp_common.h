@@ -12,6 +12,13 @@ constexpr int kHeadDim = 128;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// What raw scores, the matrix cores', are multiplied by.  Hidden ones are -inf before that, and a factor of 0 (softmax_scale = 0: all visible keys
+// weigh the same) would make them NaN.  The smallest float keeps them hidden, and takes every other score, below 2^128, to less than 2^-20.
+inline float score_factor(float softmax_scale) {
+    const float f = softmax_scale * kLog2e;
+    return f == 0.f ? 1.401298464e-45f : f;
+}
+
 // Records a message for esp_last_error() and returns `code`.
 esp_status fail(esp_status code, const char* fmt, ...);
 // Returns ESP_OK or converts the pending launch error into ESP_ERR_HIP.

@@ -1460,7 +1460,7 @@ esp_status launch_prefill(const void* q, const void* k, const void* v, const int
     a.kv_slot = kv_slot;
     a.retain_slot = retain_slot; a.k_pool = (uint16_t*)k_pool; a.v_pool = (uint16_t*)v_pool;
     a.batch = batch; a.Tq = Tq; a.Tkv = Tkv; a.Hq = Hq; a.Hkv = Hkv; a.causal = causal ? 1 : 0;
-    a.scale_log2 = softmax_scale * kLog2e;
+    a.scale_log2 = score_factor(softmax_scale);
     a.G = Hq / Hkv;
     a.inv_G = 1.0f / (float)a.G;
     a.q_odd = ((uintptr_t)q & 15) != 0;
