@@ -352,7 +352,9 @@ esp_status esp_partial_attn_prefill_pool_direct(
  *   slot_idx[seq_offsets[b] .. seq_offsets[b+1])
  * (no mask).  The result is that of esp_partial_attn_decode on the two lists put
  * together, up to the order of fp32 additions and one rounding of the weights.  Either list may be
- * empty; a request that has neither gives O = 0, LSE = -inf.
+ * empty; a request that has neither gives O = 0, LSE = -inf.  An infinity in V shows as itself
+ * in the elements of O that see it (with prefix_total = 0 the call is esp_partial_attn_decode, which
+ * may show NaN there).
  *
  *   group_offsets int32 [n_groups+1]: requests of group g, from 0 to B;
  *   prefix_offsets int32 [n_groups+1], from 0 to prefix_total; prefix_slots int32 [prefix_total].

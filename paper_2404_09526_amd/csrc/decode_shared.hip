@@ -86,6 +86,7 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
         Columns::PFrag pf[2];
         cols.weigh(sc, scale_log2, pf);
         if (next) wait_vm<8>(); else wait_vm<0>();
+        if (rows < 32) Columns::clear_v(lds_k, rows, lane);         // (the list's last tile)
         cols.accumulate(pf);
         if (next) fetch_v();
     }
@@ -318,10 +319,14 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
             Columns::PFrag pf[2];
             if (n_rows > 0) {
                 const int here = seg - i * STEP - team * 32;
-                if (here < 32) {                                    // keys past the end are hidden
+                if (here < 32) {                                    // keys past the end are hidden, and their V, the last row's again, is 0 (as 0 times an infinity is not)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) sc[r] = -INFINITY;
+                        if (8 * (r >> 2) + 4 * hi + (r & 3) >= here) {
+                            sc[r] = -INFINITY;
+#pragma unroll
+                            for (int db = 0; db < 4; ++db) vf[4 * (r >> 3) + db].s[(r >> 2) & 1][r & 3] = 0;   // (that key's element of the operands)
+                        }
                 }
                 // Probabilities against the offset in use, without a look at the scores first; their sums tell whether it has to move.
                 float sum, sum_r;
@@ -528,6 +533,7 @@ __global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(Share
         Columns::PFrag pf[2];
         cols.weigh(sc, scale_log2, pf);
         if (next) wait_vm<8>(); else wait_vm<0>();
+        if (here < 32) Columns::clear_v(lds_k, here, lane);         // (the list's last tile)
         cols.accumulate(pf);
         if (next) {
             fetch(lds_k + kColKBytes, vbase, slots_next, false);
