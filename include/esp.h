@@ -360,13 +360,16 @@ esp_status esp_partial_attn_prefill_pool_direct(
  *   prefix_offsets int32 [n_groups+1], from 0 to prefix_total; prefix_slots int32 [prefix_total].
  *   max_prefix, max_group: upper bounds of a prefix's tokens and of a group's
  *     requests (host-known).  A request past max_group of its group is left
- *     without the prefix.
+ *     without the prefix, a prefix longer than max_prefix is read as far as that.
  *   Everything else as in esp_partial_attn_decode (max_len: of the requests' own
  *   lists).  B = 0 writes nothing.  n_groups = 0 needs prefix_total = 0: the group arrays may
  *   then be NULL.
  *   q, the pools and O lie on 16 bytes (ESP_ERR_INVALID_ARG).
  *   workspace: at least esp_decode_shared_workspace_bytes(...) bytes, 256-byte
  *   aligned; contents need not be preserved.  0 from there: the call would be refused.
+ *   That rises with every size but the heads (a block for the largest step is large
+ *   enough for all smaller ones), and beyond 128 MiB for the prefixes and as much for the own tokens only as
+ *   ranges of 4096 keys of the one and 512 of the other need: a row of 520 Hq bytes for each range of each request.
  * With esp_debug_set_validate the two lists and three offset arrays are checked as
  * in esp_partial_attn_decode.
  */

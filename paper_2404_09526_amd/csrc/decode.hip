@@ -228,6 +228,22 @@ size_t decode_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq, int32
     return want > least ? want : least;
 }
 
+// A bound that rises with both sizes.  `kept` is no more than kDecMaxWG, nor than total_tokens in its shortest ranges; decode_range makes no more ranges than `kept`,
+// or than the block has room for beside B, nor shorter ones than its least.
+size_t decode_workspace_bound(int32_t B, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    const bool burst = decode_burst_layout(Hq, Hkv);
+    const int64_t nt = !burst ? 1 : Hkv >= 32 ? 1 : kDecWaves / (Hkv / 4), step = burst ? nt * kDecTB : kGqWaves * 32, shortest = burst ? 2 * step : step;
+    auto upto = [&](int64_t range) { return ((int64_t)total_tokens + range - 1) / range; };
+    int64_t kept = upto(burst ? 8 * step : 512);
+    if (kept > kDecMaxWG) kept = kDecMaxWG;
+    if (kept < 1) kept = 1;
+    const int64_t block = (int64_t)ESP_DECODE_STATIC_SCRATCH_BYTES / partial_bytes(Hq), finest = upto(shortest) + 1 + B;
+    int64_t want = kept + B > block ? kept + B : block;
+    if (want > finest) want = finest;
+    const int64_t least = (kept + B) * nt;
+    return (size_t)(want > least ? want : least) * (size_t)partial_bytes(Hq) + 256;
+}
+
 // Bound by HBM.  A step is a chain: slots, rows (8 KiB a wavefront), products.  The chains of two steps overlap: rows are
 // loaded a step ahead and slots two (scalar loads: they do not queue behind the rows), in registers that still leave room
 // for two workgroups per CU.  The wavefronts that share a head block (rows of less than 8 KiB) leave one partial together;

@@ -34,9 +34,10 @@ constexpr int kWholeWaves = 8;                                      // of a work
 // probabilities change nothing for their bf16 or the fp32 sums.
 constexpr float kSharedSum = 4096.f;
 
-// Partials of ranges of `range` keys: accumulators [slots][rows][128], then (maximum, sum) pairs [slots][rows]; those of list b, whose first token is s0, lie
-// from slot s0 / range + b on.  Rows: max_group Hq of a prefix, Hq of a request.
-struct SharedParts { float* acc; float* ml; int32_t range; };
+// Partials of ranges of `range` keys: accumulators [rows][128], then (maximum, sum) pairs [rows], a row to a query head.  Those of a list that begins at token s0
+// lie from slot s0 / range + (the list's number) on, a slot being Hq rows of a request, or of a prefix max_group times as many.  So groups of very different
+// size would take the largest's room for every range; then a prefix's lie by request, `each` of Hq rows to one, as many as the longest prefix has (0: by slot).
+struct SharedParts { float* acc; float* ml; int32_t range, each; };
 // The work of the first launch: `prefix` workgroups on the prefix (units (range, KV head), `blocks` column blocks each) and `own` on the requests' own
 // rows, in eights: among the first `first` eights first_prefix are the prefix's, up to number `mixed` the rest of those, spread evenly both times; own rows alone
 // come last.
@@ -94,9 +95,11 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
 
 // Ranges counted from each list's first token on (lists: offsets[b] .. offsets[b + 1]), all whole ones first, then what is left of each list: where
 // range i is, as request_range (esp_common.h) finds it, but 64 N lists at a time, whose offsets are one round trip for both kinds where that is all.
-// members: offsets of something else by list, whose bounds for the list that is found go to m0 and m1 (asked for together with its own).
+// longest: tokens of a list that count.  members: offsets of something else by list, whose bounds for the list that is found go to m0 and m1 (asked for together
+// with its own).
+struct ListRange { int32_t b, t0, t1, part, w; };                   // list; tokens; number within the list, and along all (s0 / range + part)
 template <int N>
-__device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int lane, const int32_t* members, int32_t& m0, int32_t& m1) {
+__device__ __forceinline__ ListRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int32_t longest, int lane, const int32_t* members, int32_t& m0, int32_t& m1) {
     int32_t s0[N], s1[N], of0[N], of1[N];
 #pragma unroll 1
     for (int rest = 0; rest < 2; ++rest) {
@@ -113,8 +116,8 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 if (base + 64 * u >= B) break;
-                const int32_t whole = (uint32_t)max(s1[u] - s0[u], 0) / (uint32_t)range;
-                const int32_t n = base + 64 * u + lane >= B ? 0 : rest ? (s1[u] - s0[u] > whole * range ? 1 : 0) : whole;
+                const int32_t len = min(max(s1[u] - s0[u], 0), longest), whole = (uint32_t)len / (uint32_t)range;
+                const int32_t n = base + 64 * u + lane >= B ? 0 : rest ? (len > whole * range ? 1 : 0) : whole;
                 int32_t upto = n;
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) {
@@ -124,17 +127,17 @@ __device__ __forceinline__ RequestRange find_range(int32_t i, int32_t range, int
                 const uint64_t hit = __builtin_amdgcn_ballot_w64(upto > i);
                 if (hit) {
                     const int l = __builtin_ctzll(hit);
-                    const int32_t start = __builtin_amdgcn_readlane(s0[u], l), end = __builtin_amdgcn_readlane(s1[u], l);
+                    const int32_t start = __builtin_amdgcn_readlane(s0[u], l), left = __builtin_amdgcn_readlane(len, l);
                     const int32_t part = rest ? __builtin_amdgcn_readlane(whole, l) : i - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
                     const int32_t t0 = start + part * range;
                     if (members) { m0 = __builtin_amdgcn_readlane(of0[u], l); m1 = __builtin_amdgcn_readlane(of1[u], l); }
-                    return {base + 64 * u + l, t0, t0 + min(range, end - t0), start / range + part};
+                    return {base + 64 * u + l, t0, t0 + min(range, left - part * range), part, start / range + part};
                 }
                 i -= __builtin_amdgcn_readlane(upto, 63);
             }
         }
     }
-    return {0, 0, 0, 0};                                            // the launch is an upper bound
+    return {0, 0, 0, 0, 0};                                            // the launch is an upper bound
 }
 
 // The requests' own rows: a wavefront alone on (a range of a request, KV head, up to 32 of its query heads), heads next to each other as in a
@@ -146,7 +149,7 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
     const uint32_t unit = (uint32_t)index * WAVES + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
     const int kvh = rest / (uint32_t)chunks, g0 = (rest - kvh * chunks) * 32, ng = min(32, G - g0), h0 = kvh * G + g0;
     int32_t none;
-    const RequestRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, lane, nullptr, none, none);
+    const ListRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, INT32_MAX, lane, nullptr, none, none);
     const int32_t seg = min(at.t1, a.total_tokens) - at.t0;         // (never past the slot list)
     if (seg <= 0) return;
     int32_t* const list = (int32_t*)(smem + 2 * SharedGeometry<WAVES>::half) + wave * SharedGeometry<WAVES>::own;
@@ -185,14 +188,14 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
 // of the scores, V's one step ahead of their products, and each has a ring of COLS stages (16 KiB a wavefront together): group j of transfers is V of step j
 // and K of step j + 1.
 // A team of one wavefront shares nothing: it waits for its own rows only (sweep_tiles).
-struct PrefixPart { RequestRange at; int32_t b0, seg, n_all, kvh; };  // a range of group at.b's prefix: its keys, the group's first request and packed rows
+struct PrefixPart { ListRange at; int32_t b0, seg, n_all, kvh; };  // a range of group at.b's prefix: its keys, the group's first request and packed rows
 template <int WAVES, int COLS, bool ONCE>
 __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_log2, const SharedParts& parts, const PrefixPart& part, uint32_t cb, unsigned char* smem,
                                               int wave, int lane) {
     constexpr int TEAMS = WAVES / COLS, STEP = 32 * TEAMS, MOVES = 8 / COLS;   // MOVES: a wavefront's transfers of K, and of V, of a tile
     const int team = wave / COLS, ct = wave % COLS;
     const int qi = lane & 31, hi = lane >> 5;
-    const RequestRange& at = part.at;
+    const ListRange& at = part.at;
     const int32_t t0 = at.t0, b0 = part.b0, seg = part.seg, n_all = part.n_all, kvh = part.kvh, G = a.Hq / a.Hkv;
     if (n_all <= (int32_t)cb * (32 * COLS)) return;
     const int32_t rho0 = cb * (32 * COLS) + ct * 32, n_rows = n_all - rho0;   // (columns of this wavefront, up to 32; none: it only moves tiles)
@@ -402,7 +405,8 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
         if (hi == 0) ((float2*)(smem + WAVES * kColWaveBytes))[wave * 32 + qi] = make_float2(cols.m, l);
     }
     __syncthreads();
-    const int64_t slot = (int64_t)(at.w + at.b) * a.max_group * a.Hq;
+    // the range's rows for the group's first request, and how far apart those of two requests lie
+    const int64_t slot = (parts.each ? (int64_t)b0 * parts.each + at.part : (int64_t)(at.w + at.b) * a.max_group) * a.Hq, apart = (int64_t)(parts.each ? parts.each : 1) * a.Hq;
 #pragma unroll 1
     for (int i = 0; i < kRowPairs; ++i) {
         const int in = (wave * kRowPairs + i) * 2 + hi;              // of the workgroup's 32 COLS columns
@@ -427,7 +431,7 @@ __device__ __forceinline__ void shared_prefix(const SharedArgs& a, float scale_l
             out.x += x.x * c; out.y += x.y * c; out.z += x.z * c; out.w += x.w * c;
         }
         const int32_t req = col / G;
-        const int64_t ph = slot + req * a.Hq + kvh * G + (col - req * G);
+        const int64_t ph = slot + req * apart + kvh * G + (col - req * G);
         ((float4*)(parts.acc + ph * kHeadDim))[qi] = out;
         if (qi == 0) *(float2*)(parts.ml + ph * 2) = make_float2(mx, lsum);
     }
@@ -455,7 +459,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void shared_partial_kernel(SharedArg
     part.kvh = unit % (uint32_t)a.Hkv;
     int32_t b1 = 0;
     part.b0 = 0;
-    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, lane, a.group_offsets, part.b0, b1);
+    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, a.max_prefix, lane, a.group_offsets, part.b0, b1);
     part.n_all = min(min(b1, a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
     part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
     if (part.seg <= 0 || part.n_all <= 0) return;
@@ -486,7 +490,7 @@ __global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(Share
         if (!hit) continue;
         const int l = __builtin_ctzll(hit);
         p0 = __builtin_amdgcn_readlane(from, l);
-        if (b - __builtin_amdgcn_readlane(g0, l) < a.max_group) P = max(__builtin_amdgcn_readlane(to, l) - p0, 0);
+        if (b - __builtin_amdgcn_readlane(g0, l) < a.max_group) P = min(max(__builtin_amdgcn_readlane(to, l) - p0, 0), a.max_prefix);
         break;
     }
     const uint32_t n = (uint32_t)P + max(s1 - s0, 0);               // (without a sign: tiles that are looked ahead to may start past 2^31)
@@ -591,8 +595,8 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
         const int l = __builtin_ctzll(hit);
         const int32_t b0 = __builtin_amdgcn_readlane(g0, l), from = __builtin_amdgcn_readlane(p0, l), to = __builtin_amdgcn_readlane(p1, l);
         if (b - b0 < a.max_group && to > from) {
-            const int64_t rows = (int64_t)a.max_group * a.Hq;
-            add(parts.acc, parts.ml, (int64_t)(from / parts.range + base + l) * rows + (int64_t)(b - b0) * a.Hq + h, rows, (to - from - 1) / parts.range + 1);
+            const int64_t first = parts.each ? (int64_t)b * parts.each : (int64_t)(from / parts.range + base + l) * a.max_group + (b - b0);
+            add(parts.acc, parts.ml, first * a.Hq + h, (int64_t)(parts.each ? 1 : a.max_group) * a.Hq, (min(to - from, a.max_prefix) - 1) / parts.range + 1);
         }
         break;
     }
@@ -634,10 +638,43 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
     if (lane == 0) a.LSE[pair] = Lt == 0.f ? -INFINITY : (mx + __builtin_amdgcn_logf(Lt)) * kLn2;
 }
 
+// The sizes of a call, and what its partials take.
+struct SharedSizes {
+    int32_t B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv;
+    // Of so many times Hq rows: whole 256 bytes, and no more than 2^60 of them (such a call is refused).
+    size_t bytes(int64_t times) const {
+        const double all = (double)times * Hq * ((kHeadDim + 2) * sizeof(float));
+        return all > 0x1p60 ? (size_t)1 << 60 : ((size_t)times * Hq * ((kHeadDim + 2) * sizeof(float)) + 255) / 256 * 256;
+    }
+    // Of the prefixes in ranges of so many keys, by request (to `each`) or by slot (0), whichever is less: a group's requests times its ranges, summed over all groups, can
+    // be no more than either.
+    int64_t prefix_rows(int32_t range, int32_t* each = nullptr) const {
+        const int64_t most = ((int64_t)max_prefix + range - 1) / range, by_request = B * most, slots = (int64_t)prefix_total / range + n_groups;
+        const bool by_slot = (double)slots * max_group < (double)by_request;
+        if (each) *each = by_slot ? 0 : (int32_t)most;
+        return by_slot ? slots * max_group : by_request;
+    }
+    int64_t own_rows(int32_t range) const { return total_tokens == 0 ? 0 : (int64_t)total_tokens / range + B; }   // (of requests of any lengths)
+    // Room for them: for the shortest ranges, but beyond kRoom no more than the longest need.  It rises with every size, so a block that a call fits is large enough for all
+    // smaller ones; the plan takes ranges that fit.  (Of 3000 drawn batches none would take others with more room; with 64 MiB 38 would, the worst for 20 % of its estimate.)
+    static constexpr size_t kRoom = (size_t)128 << 20;
+    static constexpr int32_t kLeast = 32, kMost = 4096, kOwnLeast = 64, kOwnMost = 512;   // keys of a range
+    static size_t room(size_t most, size_t least) { return most < kRoom ? most : least > kRoom ? least : kRoom; }
+    size_t prefix_room() const { return room(bytes(prefix_rows(kLeast)), bytes(prefix_rows(kMost))); }
+    size_t own_room() const { return room(bytes(own_rows(kOwnLeast)), bytes(own_rows(kOwnMost))); }
+    bool alone() const { return prefix_total == 0 || max_prefix == 0 || max_group == 0; }   // no prefix: the plain decode
+    size_t workspace() const {
+        const size_t plain = decode_workspace_bound(B, total_tokens, Hq, Hkv);
+        if (alone()) return plain;
+        const size_t all = prefix_room() + own_room();
+        return all > plain ? all : plain;
+    }
+};
+
 // The ranges of both kinds, and the workgroups that they are.
 struct SharedPlan {
     int32_t range, own_range;                                       // keys of a range
-    size_t slots, own_slots;                                        // partials: of the prefix (max_group Hq rows each), of the requests' own (Hq rows each)
+    int32_t each;                                                   // partials of the prefix by request, or by slot (SharedParts)
     int64_t units, blocks, own;                                     // (range, KV head) pairs, column blocks of each; workgroups on own rows
     double us;                                                      // the estimate
     int waves, kind;                                                // of a workgroup: wavefronts, column tiles for an average group (2^kind)
@@ -653,13 +690,16 @@ constexpr double kOneAfter = 1.6;
 // from the best on average.  Four wavefronts at their best were the better by 6 % on average; eight were it for few long ranges (3 + 18 + 2 requests behind 47634, 102 and 3466 tokens,
 // 32 / 4 heads, 30 us with eight, 44 with four; 16 behind 130000, 32 / 8, 115 and 127) and by 2 % for much work of more than 128 columns and nothing else.  So
 // eight are taken where their estimate is 6 %, with more than 128 columns 8 %, the less (where it is less at all: 2 .. 3 % more time on average).
-static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+static SharedPlan shared_plan_for(int waves, const SharedSizes& of) {
+    const int32_t B = of.B, n_groups = of.n_groups, prefix_total = of.prefix_total, max_group = of.max_group, total_tokens = of.total_tokens, Hq = of.Hq, Hkv = of.Hkv;
     constexpr double kOwnStart = 5.5, kOwnTile = 3.6, kTail = 0.15, kTailOwn = 0.44, kTailBoth = 0.23, kFewRounds = 3, kWholeRound = 1.1, kPartial = 0.0055, kBytesPerUs = 5.95e6;
     constexpr double kAlone = 0.43, kBlocks = 0.865;                // of a step's time: on a chip that is hardly filled; where blocks of four tiles find rows in the L2
     struct Times { double start, step; };
     constexpr Times kTimes[4] = {{5.6, 4.15}, {12.1, 1.57}, {8.3, 1.48}, {15.5, 1.04}};   // of a workgroup with 1, 2, 4, 8 column tiles
-    constexpr int32_t kRanges[] = {32, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, 4096}, kOwnRanges[] = {64, 128, 192, 256, 384, 512};
+    constexpr int32_t kRanges[] = {SharedSizes::kLeast, 64, 128, 256, 384, 512, 768, 1024, 1536, 2048, SharedSizes::kMost};
+    constexpr int32_t kOwnRanges[] = {SharedSizes::kOwnLeast, 128, 192, 256, 384, SharedSizes::kOwnMost};
     static_assert(kRanges[10] == SharedGeometry<4>::most && kRanges[10] == SharedGeometry<8>::most && kOwnRanges[5] == SharedGeometry<4>::own, "their slots lie in LDS");
+    const size_t room = of.prefix_room(), own_room = of.own_room();
     SharedPlan p = {};
     const int64_t G = Hq / Hkv, chunks = (G + 31) / 32, mean = n_groups > 1 ? (B + n_groups / 2) / n_groups : max_group, rows = (mean > 1 ? mean : 1) * G;
     const int cols = shared_cols(rows, waves), kind = __builtin_ctz(cols);
@@ -670,9 +710,11 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
     auto own_wgs = [&](int32_t range) { return total_tokens == 0 ? 0 : (((int64_t)total_tokens / range + B) * Hkv * chunks + waves - 1) / waves; };
     p.us = HUGE_VAL;
     for (const int32_t range : kRanges) {
+        if (of.bytes(of.prefix_rows(range)) > room) continue;       // (the longest fits)
         const double wgs = (ceil((double)prefix_total / range) + 0.5 * (n_groups - 1)) * wide;
         const double steps = (double)((range + step - 1) / step) * (kind == 2 && rows > 128 ? kBlocks : 1);
         for (const int32_t own_range : kOwnRanges) {
+            if (of.bytes(of.own_rows(own_range)) > own_room) continue;
             const double own = (double)own_wgs(own_range), n = wgs + own, full = kAlone + (1 - kAlone) * fmin(1, n / at_once);
             const double one = kTimes[kind].start + kTimes[kind].step * steps * full, prefix_us = wgs * one;
             const double mine = kOwnStart + kOwnTile * full * own_range / 32, longest = total_tokens == 0 ? one : fmax(one, mine);
@@ -692,24 +734,18 @@ static SharedPlan shared_plan_for(int waves, int32_t B, int32_t n_groups, int32_
     p.waves = waves;
     p.kind = kind;
     p.blocks = (max_group * G + 32 * waves - 1) / (32 * waves);     // (fewer column tiles than wavefronts are one block)
-    p.slots = (size_t)(prefix_total / p.range) + n_groups;
-    p.units = (int64_t)p.slots * Hkv;
+    p.units = ((int64_t)(prefix_total / p.range) + n_groups) * Hkv;
+    of.prefix_rows(p.range, &p.each);
     p.own = own_wgs(p.own_range);
-    p.own_slots = (size_t)(total_tokens / p.own_range + B);         // (of requests of any lengths)
     return p;
 }
-static SharedPlan shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    const SharedPlan four = shared_plan_for(4, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
-    const SharedPlan eight = shared_plan_for(8, B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv);
+static SharedPlan shared_plan(const SharedSizes& of) {
+    const SharedPlan four = shared_plan_for(4, of), eight = shared_plan_for(8, of);
     return eight.us * (eight.kind == 3 ? 1.08 : 1.06) < four.us ? eight : four;
 }
-static size_t partials_bytes(size_t slots, int64_t rows) { return (slots * rows * (kHeadDim + 2) * sizeof(float) + 255) / 256 * 256; }
-static size_t partials_bytes(const SharedPlan& p, int32_t max_group, int32_t Hq) { return partials_bytes(p.slots, (int64_t)max_group * Hq) + partials_bytes(p.own_slots, Hq); }
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
                                      int32_t Hq, int32_t Hkv) {
-    (void)max_prefix;
-    if (prefix_total == 0 || max_group == 0) return decode_workspace_bytes(B, total_tokens, Hq, Hkv);
-    return partials_bytes(shared_plan(B, n_groups, prefix_total, max_group, total_tokens, Hq, Hkv), max_group, Hq);
+    return SharedSizes{B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv}.workspace();
 }
 
 // Which calls run in one launch: those with no more workgroups than CUs whose estimate is the less.  In one launch: a start and an end, then the longest
@@ -755,15 +791,14 @@ static SharedWork shared_order(const SharedPlan& p, int64_t prefix, int64_t own)
 }
 
 esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    const bool alone = a.prefix_total == 0 || a.max_group == 0;     // no prefix: the plain decode
+    const SharedSizes of = {a.B, a.n_groups, a.prefix_total, a.max_prefix, a.max_group, a.total_tokens, a.Hq, a.Hkv};
     if ((int64_t)a.B * a.Hq > INT32_MAX) return fail(ESP_ERR_INVALID_ARG, "decode (shared): too many rows for one launch");
-    SharedPlan p = {};
-    if (!alone) p = shared_plan(a.B, a.n_groups, a.prefix_total, a.max_group, a.total_tokens, a.Hq, a.Hkv);
-    const size_t need = alone ? decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv) : partials_bytes(p, a.max_group, a.Hq);
+    const size_t need = of.workspace();
     if (workspace_bytes < need) return fail(ESP_ERR_WORKSPACE, "decode (shared): workspace needs %zu bytes, got %zu", need, workspace_bytes);
-    if (alone)
+    if (of.alone())                                                 // (on what that call asks for, so that the larger block changes nothing)
         return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
-                             workspace, need, stream);
+                             workspace, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream);
+    const SharedPlan p = shared_plan(of);
     if (shared_whole(a, p)) {
         const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
         if (a.B > (int32_t)(UINT32_MAX / (kWholeWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
@@ -775,10 +810,11 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t wor
     const int64_t prefix = (p.units + 7) / 8 * 8 * p.blocks, own = (p.own + 7) / 8 * 8;
     if (prefix + own > (int64_t)(UINT32_MAX / (p.waves * 64)) || p.units > INT32_MAX / 2)
         return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many heads, requests or groups for one launch");
+    const int64_t rows = of.prefix_rows(p.range), own_rows = of.own_rows(p.own_range);
     float* const acc = (float*)workspace;
-    const SharedParts parts = {acc, acc + p.slots * a.max_group * a.Hq * kHeadDim, p.range};
-    float* const own_acc = (float*)((char*)workspace + partials_bytes(p.slots, (int64_t)a.max_group * a.Hq));
-    const SharedParts mine = {own_acc, own_acc + p.own_slots * a.Hq * kHeadDim, p.own_range};
+    const SharedParts parts = {acc, acc + rows * a.Hq * kHeadDim, p.range, p.each};
+    float* const own_acc = (float*)((char*)workspace + of.bytes(rows));
+    const SharedParts mine = {own_acc, own_acc + own_rows * a.Hq * kHeadDim, p.own_range, 0};
     const SharedWork work = shared_order(p, prefix, own);
     const dim3 grid((unsigned)(prefix + own)), block(p.waves * 64);
     if (p.waves == 8) hipLaunchKernelGGL(shared_partial_kernel<8>, grid, block, 0, stream, a, score_factor(a.softmax_scale), parts, mine, work);

@@ -88,6 +88,9 @@ esp_status launch_decode(const void* q, const void* k_pool, const void* v_pool, 
                          int32_t Hkv, float softmax_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes,
                          hipStream_t stream, const MergeArgs* peers = nullptr, int32_t n_peers = 0);
 
+// no less than decode_workspace_bytes of any call of up to so many requests and tokens (that may fall as they grow)
+size_t decode_workspace_bound(int32_t B, int32_t total_tokens, int32_t Hq, int32_t Hkv);
+
 // block tables and slot lists (slots.hip); free entries, rows and widths of the table in entries
 esp_status launch_extend_table(const int32_t* free_pages, int32_t n_free, const int32_t* req_row, const int32_t* old_lens, const int32_t* new_lens,
                                int32_t B, int32_t page, int32_t* table, int32_t rows, int32_t width, int32_t* taken, hipStream_t stream);
