@@ -86,13 +86,6 @@ struct Columns {
         }
         l += psum; l_r += psum_r;
     }
-    // V has landed, in a tile of which only `rows` rows are keys and the others repeat the last: those have weight 0, and become 0 here, as 0 times an
-    // infinity is not.
-    static __device__ __forceinline__ void clear_v(uint32_t lds_k, int rows, int lane) {
-        for (int r = rows + (lane >> 4); r < 32; r += 4)
-            *(ESP_LDS u32x4*)(uintptr_t)(lds_k + kColKBytes + r * 256 + (lane & 15) * 16) = u32x4{0u, 0u, 0u, 0u};
-        asm volatile("" ::: "memory");                              // (before the reads that follow: a wavefront's LDS instructions keep their order)
-    }
     // V has landed: O^T += V^T P^T, 16 keys per step.  The tile's LDS reads are complete when this returns.
     __device__ __forceinline__ void accumulate(const PFrag (&pf)[2]) {
 #pragma unroll

@@ -50,6 +50,10 @@ struct SharedWork {
     }
 };
 
+// V of the rows past the end of a tile that is not full.  K's repeat the last row, and their weight is 0: of V that would not do, as 0 times an infinity is not 0.
+// (Cleared in LDS when V had landed, the call of four short requests took 0.2 us more.)
+__device__ const u32x4 kZeroRow[kHeadDim / 8] = {};
+
 // A wavefront on tiles of 32 keys of its own, number `first`, first + step, ...: their rows go to its block of the LDS, the next tile's K as soon
 // as this one's scores are taken, its V as soon as this one's has been read.  list: the slots of all `seg` keys, in LDS (a load of them on the way would
 // be waited for with everything that was asked for before it).
@@ -63,13 +67,18 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
 #pragma unroll
         for (int n = 0; n < 8; ++n) load_to_lds_b128_at_nt(lds_k + 1024 * n, kbase + ((uint64_t)slot[n] * row_bytes + col_k_within(n, lane)));
     };
-    auto fetch_v = [&] {
+    auto fetch_v = [&](int i) {
+        const int rows = seg - 32 * i;
 #pragma unroll
-        for (int n = 0; n < 8; ++n) load_to_lds_b128_at_nt(lds_k + kColKBytes + 1024 * n, vbase + ((uint64_t)slot[n] * row_bytes + col_v_within(lane)));
+        for (int n = 0; n < 8; ++n) {
+            const char* from = vbase + ((uint64_t)slot[n] * row_bytes + col_v_within(lane));
+            if (rows < 32 && col_row(n, lane) >= rows) from = (const char*)kZeroRow + col_v_within(lane);
+            load_to_lds_b128_at_nt(lds_k + kColKBytes + 1024 * n, from);
+        }
     };
     if (32 * first >= seg) return;
     fetch_k(first);
-    fetch_v();
+    fetch_v(first);
     for (int i = first; 32 * i < seg; i += step) {
         const int rows = min(32, seg - 32 * i);
         const bool next = 32 * (i + step) < seg;
@@ -87,9 +96,8 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
         Columns::PFrag pf[2];
         cols.weigh(sc, scale_log2, pf);
         if (next) wait_vm<8>(); else wait_vm<0>();
-        if (rows < 32) Columns::clear_v(lds_k, rows, lane);         // (the list's last tile)
         cols.accumulate(pf);
-        if (next) fetch_v();
+        if (next) fetch_v(i + step);
     }
 }
 
@@ -514,12 +522,16 @@ __global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(Share
     Columns cols;
     cols.place(lds_k, lane);
     cols.clear();
-    auto fetch = [&](uint32_t to, const char* base, int32_t of, bool is_k) {
+    auto fetch = [&](uint32_t to, const char* base, int32_t of, uint32_t i, bool is_k) {
+        const uint32_t rows = n - 32 * i;                           // of the tile, or more
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-            load_to_lds_b128_at(to + 1024 * x, base + ((uint64_t)(uint32_t)__shfl(of, col_row(x, lane)) * row_bytes + (is_k ? col_k_within(x, lane) : col_v_within(lane))));
+        for (int x = 0; x < 8; ++x) {
+            const char* from = base + ((uint64_t)(uint32_t)__shfl(of, col_row(x, lane)) * row_bytes + (is_k ? col_k_within(x, lane) : col_v_within(lane)));
+            if (!is_k && rows < 32 && col_row(x, lane) >= (int)rows) from = (const char*)kZeroRow + col_v_within(lane);
+            load_to_lds_b128_at(to + 1024 * x, from);
+        }
     };
-    if (32 * wave < n) { fetch(lds_k, kbase, slots, true); fetch(lds_k + kColKBytes, vbase, slots, false); }
+    if (32 * wave < n) { fetch(lds_k, kbase, slots, wave, true); fetch(lds_k + kColKBytes, vbase, slots, wave, false); }
     for (uint32_t i = wave; 32 * i < n; i += kWholeWaves) {
         const int here = min(32u, n - 32 * i);
         const bool next = 32 * (i + kWholeWaves) < n;
@@ -527,7 +539,7 @@ __global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(Share
         floatx16 sc = cols.scores(qf);
         if (next) {
             asm volatile("" :: "v"(sc));                            // K has been read
-            fetch(lds_k, kbase, slots_next, true);
+            fetch(lds_k, kbase, slots_next, i + kWholeWaves, true);
         }
         if (here < 32) {
 #pragma unroll
@@ -537,10 +549,9 @@ __global__ __launch_bounds__(kWholeWaves * 64, 2) void shared_whole_kernel(Share
         Columns::PFrag pf[2];
         cols.weigh(sc, scale_log2, pf);
         if (next) wait_vm<8>(); else wait_vm<0>();
-        if (here < 32) Columns::clear_v(lds_k, here, lane);         // (the list's last tile)
         cols.accumulate(pf);
         if (next) {
-            fetch(lds_k + kColKBytes, vbase, slots_next, false);
+            fetch(lds_k + kColKBytes, vbase, slots_next, i + kWholeWaves, false);
             slots_next = tile_slots(i + 2 * kWholeWaves);
         }
     }
