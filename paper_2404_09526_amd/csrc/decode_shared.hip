@@ -103,11 +103,12 @@ __device__ __forceinline__ void sweep_tiles(Columns& cols, const bf16x8 (&qf)[8]
 
 // Ranges counted from each list's first token on (lists: offsets[b] .. offsets[b + 1]), all whole ones first, then what is left of each list: where
 // range i is, as request_range (esp_common.h) finds it, but 64 N lists at a time, whose offsets are one round trip for both kinds where that is all.
-// longest: tokens of a list that count.  members: offsets of something else by list, whose bounds for the list that is found go to m0 and m1 (asked for together
+// total: entries that there are (offsets past them stand for that end); longest: tokens of a list that count.  members: offsets of something else by list, whose bounds for the list that is found go to m0 and m1 (asked for together
 // with its own).
 struct ListRange { int32_t b, t0, t1, part, w; };                   // list; tokens; number within the list, and along all (s0 / range + part)
 template <int N>
-__device__ __forceinline__ ListRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int32_t longest, int lane, const int32_t* members, int32_t& m0, int32_t& m1) {
+__device__ __forceinline__ ListRange find_range(int32_t i, int32_t range, int32_t B, const int32_t* offsets, int32_t total, int32_t longest, int lane, const int32_t* members,
+                                                int32_t& m0, int32_t& m1) {
     int32_t s0[N], s1[N], of0[N], of1[N];
 #pragma unroll 1
     for (int rest = 0; rest < 2; ++rest) {
@@ -117,7 +118,7 @@ __device__ __forceinline__ ListRange find_range(int32_t i, int32_t range, int32_
 #pragma unroll
                 for (int u = 0; u < N; ++u) {
                     const int b = min(base + 64 * u + lane, B - 1);
-                    s0[u] = offsets[b]; s1[u] = offsets[b + 1];
+                    s0[u] = min(offsets[b], total); s1[u] = min(offsets[b + 1], total);
                     if (members) { of0[u] = members[b]; of1[u] = members[b + 1]; }
                 }
             }
@@ -157,8 +158,8 @@ __device__ __forceinline__ void shared_own(const SharedArgs& a, float scale_log2
     const uint32_t unit = (uint32_t)index * WAVES + wave, i = unit / (uint32_t)(a.Hkv * chunks), rest = unit - i * (uint32_t)(a.Hkv * chunks);
     const int kvh = rest / (uint32_t)chunks, g0 = (rest - kvh * chunks) * 32, ng = min(32, G - g0), h0 = kvh * G + g0;
     int32_t none;
-    const ListRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, INT32_MAX, lane, nullptr, none, none);
-    const int32_t seg = min(at.t1, a.total_tokens) - at.t0;         // (never past the slot list)
+    const ListRange at = find_range<4>(i, mine.range, a.B, a.seq_offsets, a.total_tokens, INT32_MAX, lane, nullptr, none, none);
+    const int32_t seg = at.t1 - at.t0;
     if (seg <= 0) return;
     int32_t* const list = (int32_t*)(smem + 2 * SharedGeometry<WAVES>::half) + wave * SharedGeometry<WAVES>::own;
     for (int j = lane; j < seg; j += 64) list[j] = a.slot_idx[at.t0 + j];
@@ -467,9 +468,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void shared_partial_kernel(SharedArg
     part.kvh = unit % (uint32_t)a.Hkv;
     int32_t b1 = 0;
     part.b0 = 0;
-    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, a.max_prefix, lane, a.group_offsets, part.b0, b1);
+    part.at = find_range<1>(unit / (uint32_t)a.Hkv, parts.range, a.n_groups, a.prefix_offsets, a.prefix_total, a.max_prefix, lane, a.group_offsets, part.b0, b1);
     part.n_all = min(min(b1, a.B) - part.b0, a.max_group) * (a.Hq / a.Hkv);
-    part.seg = min(part.at.t1, a.prefix_total) - part.at.t0;        // (never past the slot list)
+    part.seg = part.at.t1 - part.at.t0;
     if (part.seg <= 0 || part.n_all <= 0) return;
     if (part.n_all > 32 * WAVES) shared_prefix<WAVES, WAVES, false>(a, scale_log2, parts, part, cb, smem, wave, lane);
     else switch (shared_cols(part.n_all, WAVES)) {
@@ -577,7 +578,7 @@ __global__ __launch_bounds__(256) void shared_combine_kernel(SharedArgs a, int32
     if (at >= pairs) return;                                        // (a whole workgroup, or a pair is a wavefront and no barrier follows)
     const int pair = (int)at, g = grp % GROUPS;
     const int b = pair / a.Hq, h = pair - b * a.Hq;
-    const int32_t s0 = a.seq_offsets[b], s1 = a.seq_offsets[b + 1];
+    const int32_t s0 = a.seq_offsets[b], s1 = min(a.seq_offsets[b + 1], a.total_tokens);
     Weighted<4> sum;
     auto add = [&](const float* acc, const float* ml, int64_t first, int64_t step, int n) {
         for (int i = g; i < n; i += GROUPS * U) {

@@ -73,3 +73,20 @@ def test_slots_past_the_offsets_belong_to_no_request(cuda, form, groups, prefixe
     for name in ("prefix_slots", "slot_idx"):
         call[name] = torch.cat([call[name], spare])
     checked(call, both, cuda, "spare room", workspace=shared_workspace(call, cuda))
+
+
+@pytest.mark.parametrize("past", [3, 700])
+@pytest.mark.parametrize("groups,prefixes,lens", [([4], [300], [40, 0, 1, 77]), ([40, 3], [700, 64], [9] * 42 + [300]), ([200], [3000], [0, 5] * 99 + [5, 0])])
+def test_offsets_past_the_slots_read_none(cuda, form, groups, prefixes, lens, past):  # noqa: F811
+    """Offsets that end behind the lists, within the last range and ranges further: what is there counts, in every range of every request, and no more."""
+    call, both = shared_inputs(cuda, groups, prefixes, lens, 8, 2, 85)
+    free = np.setdiff1d(np.arange(call["k_pool"].shape[0]), np.concatenate(both))
+    bad = torch.full((5000,), int(free[0]), dtype=torch.int32, device=cuda)   # (behind the lists in memory: a row of the pool that is NaN)
+    for slots, offs in (("prefix_slots", "prefix_offsets"), ("slot_idx", "seq_offsets")):
+        n = call[slots].numel()
+        call[slots] = torch.cat([call[slots], bad])[:n]
+        call[offs] = call[offs].clone()
+        call[offs][-1] += past
+    checked(call, both, cuda, "past the end", workspace=shared_workspace(call, cuda))
+    call["max_prefix"], call["max_len"] = call["prefix_slots"].numel(), call["slot_idx"].numel()
+    checked(call, both, cuda, "past the end", workspace=shared_workspace(call, cuda))
