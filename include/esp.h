@@ -537,8 +537,8 @@ esp_status esp_fit_prefill_model(
  *   esp_debug_set_decode_plan: 1 makes every decode call of the CALLING THREAD work in
  *     ranges of the token list and combine them in a second launch, 2 in one launch, a
  *     workgroup to a request and key-value head; by default (0, and anything else) that
- *     too follows from an estimate.  Decode behind shared prefixes goes by it as well.  For
- *     tests.
+ *     too follows from an estimate.  Decode behind shared prefixes goes by it as well; 4 and 8 are
+ *     1, and there also say of how many wavefronts its workgroups are.  For tests.
  * and, changing nothing,
  *   esp_debug_prefill_plan_for: what a call of these sizes, with or without a causal
  *     mask, that keeps rows in the pool or not, with such a workspace would run on now,
@@ -546,12 +546,16 @@ esp_status esp_fit_prefill_model(
  *   esp_debug_prefill_plan: the same of a causal call that keeps no rows.
  *   esp_debug_decode_plan: 1 or 2, what a decode call of these sizes would do now (0:
  *     the sizes are not valid).  Host code.
+ *   esp_debug_decode_shared_plan: the same of a call behind shared prefixes: 2, or 4 or 8, in
+ *     ranges by workgroups of so many wavefronts; without a prefix what esp_debug_decode_plan says.
  */
 int32_t esp_debug_set_validate(int32_t on);
 int32_t esp_debug_set_prefill_sync_ticks(int32_t ticks);
 int32_t esp_debug_set_prefill_plan(int32_t plan);
 int32_t esp_debug_set_decode_plan(int32_t plan);
 int32_t esp_debug_decode_plan(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv);
+int32_t esp_debug_decode_shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group,
+                                     int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv);
 int32_t esp_debug_prefill_plan(int32_t Tq, int32_t Tkv, int32_t batch, int32_t max_q, int32_t max_kv,
                                int32_t Hq, int32_t Hkv, size_t workspace_bytes);
 int32_t esp_debug_prefill_plan_for(int32_t Tq, int32_t Tkv, int32_t batch, int32_t max_q, int32_t max_kv,

@@ -33,7 +33,7 @@ EXPORTS = (
     "esp_partial_attn_decode_static", "esp_partial_attn_prefill_retain", "esp_plan_prefill_batches_monotone",
     "esp_partial_attn_decode_merge", "esp_partial_attn_prefill_pool_direct",
     "esp_partial_attn_decode_shared", "esp_decode_shared_workspace_bytes", "esp_qk_norm_rope_append", "esp_extend_block_table",
-    "esp_build_slots",
+    "esp_build_slots", "esp_debug_decode_shared_plan",
 )
 ESP_DECODE_STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -71,6 +71,8 @@ def _load() -> ctypes.CDLL:
     L.esp_debug_set_decode_plan.restype = i32
     L.esp_debug_decode_plan.argtypes = [i32] * 5
     L.esp_debug_decode_plan.restype = i32
+    L.esp_debug_decode_shared_plan.argtypes = [i32] * 9
+    L.esp_debug_decode_shared_plan.restype = i32
     L.esp_partial_attn_prefill_retain.argtypes = [vp] * 7 + [i32] * 8 + [f32, i32, vp, vp, vp, i64, i32, vp, vp, vp, sz, vp]
     L.esp_partial_attn_prefill_retain.restype = i32
     L.esp_prefill_workspace_bytes.argtypes = [i32] * 6
@@ -234,13 +236,19 @@ def esp_debug_prefill_plan(Tq, Tkv, batch, max_q, max_kv, Hq, Hkv, workspace_byt
 
 
 def esp_debug_set_decode_plan(plan: int) -> int:
-    """Decode calls of this thread: 1 in ranges and a combination, 2 in one launch, 0 by estimate; returns the previous setting."""
+    """Decode calls of this thread: 1 in ranges and a combination (4 and 8 too, behind shared prefixes by workgroups of so many wavefronts), 2 in one launch, 0 by
+    estimate; returns the previous setting."""
     return int(lib.esp_debug_set_decode_plan(int(plan)))
 
 
 def esp_debug_decode_plan(B, total_tokens, max_len, Hq, Hkv) -> int:
     """What a decode call of these sizes does: 1 in ranges and a combination, 2 in one launch."""
     return int(lib.esp_debug_decode_plan(B, total_tokens, max_len, Hq, Hkv))
+
+
+def esp_debug_decode_shared_plan(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, max_len, Hq, Hkv) -> int:
+    """What a call behind shared prefixes of these sizes does: 2 in one launch, 4 or 8 in ranges by workgroups of so many wavefronts."""
+    return int(lib.esp_debug_decode_shared_plan(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, max_len, Hq, Hkv))
 
 
 def esp_prefill_workspace_bytes(Tq, Tkv, batch, Hq, Hkv, D) -> int:

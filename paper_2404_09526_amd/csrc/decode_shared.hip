@@ -752,6 +752,8 @@ static SharedPlan shared_plan_for(int waves, const SharedSizes& of) {
     return p;
 }
 static SharedPlan shared_plan(const SharedSizes& of) {
+    const int32_t forced = forced_decode_plan();
+    if (forced == 4 || forced == 8) return shared_plan_for(forced, of);
     const SharedPlan four = shared_plan_for(4, of), eight = shared_plan_for(8, of);
     return eight.us * (eight.kind == 3 ? 1.08 : 1.06) < four.us ? eight : four;
 }
@@ -765,14 +767,22 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
 // calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
 // 20 behind 300, 4 / 4 heads, 11.3 -> 8.5, of 300 behind 1000 11.6 -> 16.1*; 16 of 300 behind 30, 32 / 8, 14.8 -> 10.7, 16 of 20 behind 1000 15.6 -> 14.3, behind
 // 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.3 % on average, 26 % at most.
-static bool shared_whole(const SharedArgs& a, const SharedPlan& p) {
+static bool shared_whole(const SharedSizes& of, int32_t max_len, const SharedPlan& p) {
     const int32_t forced = forced_decode_plan();
+    if ((int64_t)of.max_prefix + max_len > INT32_MAX) return false; // (a request's keys and tiles are counted in 32 bits)
     if (forced != 0) return forced == 2;
-    const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
-    if (a.B * (int64_t)a.Hkv * chunks > 256) return false;
-    const double bytes = ((double)a.B * a.max_prefix + a.total_tokens) * a.Hkv * chunks * (4 * kHeadDim);
-    const double whole = 6.75 + fmax(0.0065 * ((double)a.max_prefix + a.max_len), bytes / 9e6), ranges = 4.6 + 0.82 * p.us + 1.4 * p.kind;
+    const int64_t chunks = (of.Hq / of.Hkv + 31) / 32;
+    if (of.B * (int64_t)of.Hkv * chunks > 256) return false;
+    const double bytes = ((double)of.B * of.max_prefix + of.total_tokens) * of.Hkv * chunks * (4 * kHeadDim);
+    const double whole = 6.75 + fmax(0.0065 * ((double)of.max_prefix + max_len), bytes / 9e6), ranges = 4.6 + 0.82 * p.us + 1.4 * p.kind;
     return whole < 0.97 * ranges;
+}
+
+int32_t query_decode_shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv) {
+    const SharedSizes of = {B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv};
+    if (of.alone()) return query_decode_plan(B, total_tokens, max_len, Hq, Hkv);
+    const SharedPlan p = shared_plan(of);
+    return shared_whole(of, max_len, p) ? 2 : p.waves;
 }
 
 // The order of the first launch.  Workgroups start in the order of their numbers as others end (on each XCD, and there on one shader engine after the other:
@@ -811,7 +821,7 @@ esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t wor
         return launch_decode(a.q, a.k_pool, a.v_pool, a.slot_idx, a.seq_offsets, a.B, a.total_tokens, a.max_len, a.Hq, a.Hkv, a.softmax_scale, a.O, a.LSE,
                              workspace, decode_workspace_bytes(a.B, a.total_tokens, a.Hq, a.Hkv), stream);
     const SharedPlan p = shared_plan(of);
-    if (shared_whole(a, p)) {
+    if (shared_whole(of, a.max_len, p)) {
         const int64_t chunks = (a.Hq / a.Hkv + 31) / 32;
         if (a.B > (int32_t)(UINT32_MAX / (kWholeWaves * 64)) || a.Hkv > 65535 || chunks > 65535)   // (only where a test asks for this form)
             return fail(ESP_ERR_UNSUPPORTED, "decode (shared): too many requests or heads for one launch of a workgroup each");

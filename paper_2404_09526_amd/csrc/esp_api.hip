@@ -89,7 +89,7 @@ int32_t esp_debug_set_prefill_sync_ticks(int32_t ticks) { return set_prefill_syn
 int32_t esp_debug_set_prefill_plan(int32_t plan) {
     return set_prefill_plan(plan < -ESP_MAX_PARTIALS || plan > ESP_MAX_PARTIALS ? 0 : plan);
 }
-int32_t esp_debug_set_decode_plan(int32_t plan) { return set_decode_plan(plan == 1 || plan == 2 ? plan : 0); }
+int32_t esp_debug_set_decode_plan(int32_t plan) { return set_decode_plan(plan == 1 || plan == 2 || plan == 4 || plan == 8 ? plan : 0); }
 int32_t esp_debug_decode_plan(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv) {
     if (B < 0 || total_tokens < 0 || max_len < 0 || !heads_ok(Hq, Hkv)) return 0;
     return query_decode_plan(B, total_tokens, max_len, Hq, Hkv);
@@ -361,13 +361,21 @@ esp_status esp_partial_attn_decode_merge(const void* q, const void* k_pool, cons
                          workspace, workspace_bytes, (hipStream_t)stream, &peers, n_peers);
 }
 
+static bool shared_sizes_ok(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
+    return B >= 0 && n_groups >= 0 && prefix_total >= 0 && max_prefix >= 0 && max_prefix <= prefix_total && max_group >= 0 && max_group <= B &&
+           (n_groups > 0 || prefix_total == 0) && total_tokens >= 0 && decode_heads_supported(Hq, Hkv);
+}
 size_t esp_decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group,
                                          int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, int32_t D) {
     (void)max_len;
-    if (B < 0 || n_groups < 0 || prefix_total < 0 || max_prefix < 0 || max_prefix > prefix_total || max_group < 0 || max_group > B ||
-        (n_groups == 0 && prefix_total > 0) || total_tokens < 0 || !decode_heads_supported(Hq, Hkv) || D != kHeadDim)
-        return 0;
+    if (!shared_sizes_ok(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv) || D != kHeadDim) return 0;
     return decode_shared_workspace_bytes(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv);
+}
+
+int32_t esp_debug_decode_shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens, int32_t max_len, int32_t Hq,
+                                     int32_t Hkv) {
+    if (!shared_sizes_ok(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, Hq, Hkv) || max_len < 0 || max_len > total_tokens) return 0;
+    return query_decode_shared_plan(B, n_groups, prefix_total, max_prefix, max_group, total_tokens, max_len, Hq, Hkv);
 }
 
 esp_status esp_partial_attn_decode_shared(const void* q, const void* k_pool, const void* v_pool, int64_t num_slots,

@@ -110,6 +110,8 @@ struct SharedArgs {
 };
 size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens,
                                      int32_t Hq, int32_t Hkv);
+// what such a call would do: 2, 4 or 8 (a workgroup's wavefronts), without a prefix query_decode_plan's answer
+int32_t query_decode_shared_plan(int32_t B, int32_t n_groups, int32_t prefix_total, int32_t max_prefix, int32_t max_group, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv);
 esp_status launch_decode_shared(const SharedArgs& a, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 // The request that holds token t, the last b with seq_offsets[b] <= t, and where it ends; found by a wavefront 64 candidates at a
@@ -182,8 +184,8 @@ esp_status launch_decode_whole(const void* q, const void* k_pool, const void* v_
                                int32_t B, int32_t total_tokens, int32_t Hq, int32_t Hkv, bool burst, float scale_log2, void* O, float* LSE,
                                const MergeArgs* peers, int32_t n_peers, hipStream_t stream);
 
-// whether decode calls of this thread work in ranges (1), in one launch (2), or by estimate (0); returns the previous value; and what a
-// call of these sizes would do
+// whether decode calls of this thread work in ranges (1; behind shared prefixes also 4 or 8: by workgroups of so many wavefronts), in one launch (2), or by estimate
+// (0); returns the previous value; and what a call of these sizes would do
 int32_t set_decode_plan(int32_t plan);
 int32_t forced_decode_plan();     // what was set
 int32_t query_decode_plan(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv);
