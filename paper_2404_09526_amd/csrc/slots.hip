@@ -166,12 +166,12 @@ __global__ __launch_bounds__(kSlotThreads) void build_slots_kernel(const int32_t
                         slot = {max(slot.x, -1), max(slot.y, -1), max(slot.z, -1), max(slot.w, -1)};
                     } else {
                         int32_t to[4];
-                        const int32_t last = page_of(t + 3) - p;     // entries of the four, up to 4 (0: all on one page)
-                        const int32_t entry[4] = {entries[0], entries[min(1, last)], entries[min(2, last)], entries[last]};
+                        const int32_t last = page_of(t + 3) - p;     // of the four's entries: 0 (all on one page), 1, or with pages of two or three tokens 2
+                        const int32_t entry[3] = {entries[0], entries[min(1, last)], entries[last]};
                         uint32_t at = t - p * page, of_page = 0;
 #pragma unroll
                         for (int u = 0; u < 4; ++u) {
-                            const int32_t x = of_page == 0 ? entry[0] : of_page == 1 ? entry[1] : of_page == 2 ? entry[2] : entry[3];
+                            const int32_t x = of_page == 0 ? entry[0] : of_page == 1 ? entry[1] : entry[2];
                             to[u] = x >= 0 ? (int32_t)((uint32_t)x * page + at) : -1;
                             if (++at == (uint32_t)page) { at = 0; ++of_page; }
                         }
