@@ -4,12 +4,16 @@
 // KV head, and the columns of MFMA tiles:
 //   S^T [keys x columns] = K Q^T,   O^T [128 x columns] += V^T P^T
 // against the prefix in ranges of keys, a partial (accumulator, maximum, sum) per (range, row).  With few columns the prefix is bound by the
-// memory, as the requests' own rows are, from some 200 columns on by the matrix cores; so one launch works on both, prefix ranges and own
+// memory, as the requests' own rows are, from some 200 columns on by the wavefronts' work on its tiles; so one launch works on both, prefix ranges and own
 // ranges side by side, and what bounds the one is left over by the other (shared_order).  A second launch combines the partials of both kinds.
 // Workgroups are of four wavefronts, two of them on a CU, so that one starts and ends beside the other's sweep, or of eight for long prefixes and little
 // else, which read a tile of keys once for 256 columns: which, and ranges of what length, is estimated (shared_plan).
+// Weights are rounded to bf16 for the product, as in the plain decode on the matrix cores (fp32 operands run at a sixteenth of the rate, and weights in two bf16 parts are
+// twice the product); their sum is that of the rounded ones, and accumulators, maxima and sums are fp32.  Against 64 bits the result is off by 2.3e-3 of its size, 1.7e-3
+// of it the rounding of O itself.
 // Measured: 64 requests of some 750 tokens behind 2051, 32 / 8 heads, 52 us (207 MB); 16 behind 65536, 32 / 32, 213 (1.24 GB, 5.8 TB/s); 256 in three groups behind 65549,
-// 40000 and 20011, 32 / 8, 416 (1.59 GB and 193 GFLOP); four short requests 7.5.
+// 40000 and 20011, 32 / 8, 412 (1.59 GB and 193 GFLOP); four short requests 7.3.  The plain decode on the joined lists (requests of 600 tokens each, 32 / 8 heads): 64
+// behind 2000 90.7 -> 41.5 us, 2 behind 2000 13.5 -> 12.4, 16 behind 30000 227 -> 46; nothing to share: 64 requests in groups of one behind 100 38.6 -> 45.6.
 #include <math.h>
 
 #include "column_tile.h"
@@ -698,8 +702,8 @@ constexpr double kOneAfter = 1.6;
 // a workgroup on the prefix takes a start and its steps, one on own rows a start and a time for each 32 keys of a wavefront, on a chip that they do not fill less of
 // it; all of them together, spread evenly, and at the end a part of the longest, or of what comes last (shared_order), or, where they are only a few rounds of the chip,
 // whole rounds; the longest alone; all rows at the memory's rate.  What is not known is how the groups differ: several are taken to be as large as their average.
-// Measured on 247 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 130 choices each, the estimates' choice was 5.5 %
-// from the best on average.  Four wavefronts at their best were the better by 6 % on average; eight were it for few long ranges (3 + 18 + 2 requests behind 47634, 102 and 3466 tokens,
+// Fitted to 247 batches (1 .. 250 requests in 1 .. 5 groups, prefixes of 0 .. 130000 tokens, thirteen head layouts) with up to 130 choices each; of 60 others the estimates' choice was
+// 4.8 % from the best on average, 25 % at most (3 + 10 + 52 requests behind 7798, 45217 and 197, 64 / 8 heads).  Four wavefronts at their best were the better by 6 % on average; eight were it for few long ranges (3 + 18 + 2 requests behind 47634, 102 and 3466 tokens,
 // 32 / 4 heads, 30 us with eight, 44 with four; 16 behind 130000, 32 / 8, 115 and 127) and by 2 % for much work of more than 128 columns and nothing else.  So
 // eight are taken where their estimate is 6 %, with more than 128 columns 8 %, the less (where it is less at all: 2 .. 3 % more time on average).
 static SharedPlan shared_plan_for(int waves, const SharedSizes& of) {
@@ -766,7 +770,8 @@ size_t decode_shared_workspace_bytes(int32_t B, int32_t n_groups, int32_t prefix
 // list's walk, or all lists' bytes from the caches, the prefix as often as there are requests; in ranges: what the plan says and a combination.  Measured on 280
 // calls (1 .. 32 requests behind one prefix of 30 .. 4000 tokens, five head layouts; in ranges -> in one launch, us; * stays in ranges): two requests of
 // 20 behind 300, 4 / 4 heads, 11.3 -> 8.5, of 300 behind 1000 11.6 -> 16.1*; 16 of 300 behind 30, 32 / 8, 14.8 -> 10.7, 16 of 20 behind 1000 15.6 -> 14.3, behind
-// 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.3 % on average, 26 % at most.
+// 2000 18.3 -> 22.1*; 32 of 300 behind 300, 32 / 1, 17.8 -> 14.3.  To the better form the choice loses 0.3 % on average, 26 % at most, on 60 batches that
+// it was not fitted to 0.8 %, and 33 % at most (76 requests behind 837, 24 / 3).
 static bool shared_whole(const SharedSizes& of, int32_t max_len, const SharedPlan& p) {
     const int32_t forced = forced_decode_plan();
     if ((int64_t)of.max_prefix + max_len > INT32_MAX) return false; // (a request's keys and tiles are counted in 32 bits)
