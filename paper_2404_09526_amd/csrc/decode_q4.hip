@@ -89,7 +89,7 @@ struct Q4Columns {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (16 * u + 4 * g + r >= left)
+                    if (16 * u + r >= left - 4 * g)
 #pragma unroll
                         for (int c = 0; c < NC; ++c) sc[c][u][r] = -INFINITY;
         }
@@ -130,6 +130,17 @@ struct Q4Columns {
                 sum = u + r == 0 ? p[u][r] : sum + p[u][r];
             }
         return sum;
+    }
+    // V's codes behind the tile's first `left` keys (vw as below): zeros, as 0 times an infinity, of a scale of 2^126 or 2^127, is not 0.  (The keys there are the last one
+    // again: a NaN among its scales shows in the result by that one.)
+    static __device__ __forceinline__ void hide(uint32_t (&vw)[2][4], int left, int g) {
+        if (left >= kQ4Tile) return;
+        const int mine = left - 4 * g;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * u + r >= mine) vw[u][r] = 0;
     }
     // vw[u][r]: codes of elements 8 l16 .. 8 l16 + 7 of key 4 g + r + 16 u, vs that key's scales, of which the lane's block is number `block`
     __device__ __forceinline__ void accumulate(const uint32_t (&vw)[2][4], const uint32_t (&vs)[2][4], int block, const PFrag (&pf)[NC]) {
@@ -398,7 +409,9 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_rows
                 floatx4 sc[NC][2];
                 typename Q4Columns<NC>::PFrag pf[NC];
                 cols.scores(kc, ks, sc);
-                cols.weigh(sc, (int)min(seg - j * kStep, (uint32_t)kStep) - tsub * kQ4Tile, g, scale_log2, pf);
+                const int left = (int)min(seg - j * kStep, (uint32_t)kStep) - tsub * kQ4Tile;
+                cols.weigh(sc, left, g, scale_log2, pf);
+                cols.hide(vw, left, g);
                 cols.accumulate(vw, vs, l16 >> 2, pf);
             }
             __syncthreads();
@@ -495,11 +508,13 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_kern
                     }
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile is in registers: another may come into its place
+                const int left = (int)min(seg - (tsub + j * nt) * kQ4Tile, (uint32_t)kQ4Tile);
+                cols.hide(vw, left, g);
                 if (kStages > 1 || j + 1 < n) load_tile(j + kStages);
                 floatx4 sc[NC][2];
                 typename Q4Columns<NC>::PFrag pf[NC];
                 cols.scores(kc, ks, sc);
-                cols.weigh(sc, (int)min(seg - (tsub + j * nt) * kQ4Tile, (uint32_t)kQ4Tile), g, scale_log2, pf);
+                cols.weigh(sc, left, g, scale_log2, pf);
                 cols.accumulate(vw, vs, l16 >> 2, pf);
             }
             wait_vm<0>();                                           // (the tiles past the last: nothing may land in what follows)
