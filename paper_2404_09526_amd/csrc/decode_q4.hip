@@ -82,7 +82,17 @@ struct Q4Columns {
             }
         }
     }
-    // scores of the tile's first `left` keys to weights, in bf16
+    // Of a tile's keys the first `left` count; the ones past them are the last one again.  V's codes (vw as below) become zeros there, as 0 times an infinity, of a scale of
+    // 2^126 or 2^127, is not 0.  (A NaN among its scales shows in the result by the last key itself.)
+    static __device__ __forceinline__ void hide(uint32_t (&vw)[2][4], int left, int g) {
+        if (left >= kQ4Tile) return;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * u + r >= left - 4 * g) vw[u][r] = 0;
+    }
+    // their scores to weights, in bf16
     __device__ __forceinline__ void weigh(floatx4 (&sc)[NC][2], int left, int g, float scale_log2, PFrag (&pf)[NC]) {
         if (left < kQ4Tile) {
 #pragma unroll
@@ -130,17 +140,6 @@ struct Q4Columns {
                 sum = u + r == 0 ? p[u][r] : sum + p[u][r];
             }
         return sum;
-    }
-    // V's codes behind the tile's first `left` keys (vw as below): zeros, as 0 times an infinity, of a scale of 2^126 or 2^127, is not 0.  (The keys there are the last one
-    // again: a NaN among its scales shows in the result by that one.)
-    static __device__ __forceinline__ void hide(uint32_t (&vw)[2][4], int left, int g) {
-        if (left >= kQ4Tile) return;
-        const int mine = left - 4 * g;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (16 * u + r >= mine) vw[u][r] = 0;
     }
     // vw[u][r]: codes of elements 8 l16 .. 8 l16 + 7 of key 4 g + r + 16 u, vs that key's scales, of which the lane's block is number `block`
     __device__ __forceinline__ void accumulate(const uint32_t (&vw)[2][4], const uint32_t (&vs)[2][4], int block, const PFrag (&pf)[NC]) {
@@ -402,6 +401,8 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_rows
                     }
                 }
                 wg_barrier();                                       // the step is in registers: the next may come into its place
+                const int left = (int)min(seg - j * kStep, (uint32_t)kStep) - tsub * kQ4Tile;
+                cols.hide(vw, left, g);
                 if (j + 1 < steps) {
                     bring(next);
                     next = slots_of(j + 2);
@@ -409,9 +410,7 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_rows
                 floatx4 sc[NC][2];
                 typename Q4Columns<NC>::PFrag pf[NC];
                 cols.scores(kc, ks, sc);
-                const int left = (int)min(seg - j * kStep, (uint32_t)kStep) - tsub * kQ4Tile;
                 cols.weigh(sc, left, g, scale_log2, pf);
-                cols.hide(vw, left, g);
                 cols.accumulate(vw, vs, l16 >> 2, pf);
             }
             __syncthreads();
