@@ -490,7 +490,8 @@ esp_status esp_build_slots(
  * bits are bf16 numbers; with scales of 2^126 and 2^127 the largest would be infinite), for a prefill pass over them; a slot outside the pool gives a row of
  * zeros.  k, v lie on 16 bytes.
  * esp_partial_attn_decode_q4 is esp_partial_attn_decode over such a pool, for any Hq that is a
- * multiple of Hkv.  An infinite value (of those scales) makes the elements of O that it enters infinite.  q lies on 16 bytes, O on 4.  workspace: at least
+ * multiple of Hkv.  An infinite value (of those scales) makes the elements of O that it enters infinite.  Weights times
+ * values are summed in fp32 before the division, as in all decode calls: over thousands of rows of values next to the largest that sum may pass its range.  q lies on 16 bytes, O on 4.  workspace: at least
  * esp_decode_q4_workspace_bytes(...) bytes (ESP_ERR_WORKSPACE otherwise), 256-byte aligned; it rises with every size,
  * contents need not be preserved.  Calls that may run at the same time need a workspace each.
  */

@@ -14,8 +14,10 @@
 // Values in 4 bits are exact in bf16; the weights are rounded to bf16 for the second product, as in the other decode kernels, and the sum they are
 // divided by is that of the rounded ones.
 //
-// The maximum that the weights are taken against follows the scores only when weights get large: any reference serves, and what lies between is far
-// inside the range of fp32 and bf16 alike.  That the weights' sum says so, which is needed anyway, leaves out the maximum of nearly every tile.
+// What the weights are taken against follows the scores only when weights get large: any reference serves.  It is set to 2^11 times the largest weight so far, and again
+// when a lane's eight weights pass 1 in sum, which leaves out the maximum of nearly every tile.  No weight is above 1, then, as if each tile's maximum were taken: a row that is
+// much heavier than those before it does not pass the range of fp32, whatever finite values it has.  (Against the largest weight itself, and up to 2048 times it, rows
+// above 2^116 came out infinite.)  What the weights lose at the other end is far below what fp32 and bf16 hold.
 #include <math.h>
 
 #include "decode_merge.h"
@@ -27,7 +29,8 @@ namespace esp {
 constexpr int kQ4Waves = 8;                        // wavefronts of a workgroup, at most
 constexpr int kQ4Tile = 32;                        // tokens that a wavefront works on at a time
 constexpr int kQ4MaxRanges = 1024;
-constexpr float kQ4Most = 2048.f;                  // of a lane's eight weights, before the maximum they are taken against follows the scores
+constexpr float kQ4Above = 11.f;                   // the reference's logarithm over the largest score's, when it is set
+constexpr float kQ4Most = 1.f;                     // of a lane's eight weights, before it is set again
 
 struct Q4Geom {
     int32_t hw, nt;         // heads of a workgroup, wavefronts to each
@@ -111,7 +114,7 @@ struct Q4Columns {
                 top = fmaxf(top, fmaxf(fmaxf(sc[c][1][0], sc[c][1][1]), fmaxf(sc[c][1][2], sc[c][1][3]))) * scale_log2;
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float m_new = fmaxf(m[c], top);
+                const float m_new = fmaxf(m[c], top + kQ4Above);
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - m_new);
                 m[c] = m_new;
                 l[c] *= alpha; l_r[c] *= alpha;
