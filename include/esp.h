@@ -528,8 +528,8 @@ size_t esp_decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t ma
  *     + sum over its queries t and heads h of exp(softmax_scale * q[t,h] . k[slot_idx[i], h/G] - LSE[t,h])
  * with G = Hq / Hkv, in fp32.  With positions, query t leaves out keys of kv_pos[i] > q_pos[t].
  * The LSE is that of the whole attention: a master's merged one where keys are spread over instances.
- * A query with LSE = -inf saw nothing and gives nothing; a NaN among q, K or LSE shows in the sums
- * that it enters.  The last `fresh` entries of each list are new tokens: their sums begin at 0, whatever
+ * A query with LSE = -inf saw nothing and gives nothing, whatever q holds there; a NaN among the others' q, K or LSE
+ * shows in the sums that it enters.  The last `fresh` entries of each list are new tokens: their sums begin at 0, whatever
  * their slots held.  So do all with decay = 0 (nothing is read then).
  *   q bf16 [Tq,Hq,D], LSE float [Tq,Hq]; k_pool bf16 [num_slots,Hkv,D], or (_q4) in 4 bits, slots
  *   slot_bytes apart; q_pos int32 [Tq], kv_pos int32 [total_tokens], both or neither; max_q >= every

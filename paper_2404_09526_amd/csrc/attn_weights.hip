@@ -133,7 +133,8 @@ struct OneQuery {
         for (int r = 0; r < 4; ++r) {
             asm volatile("" : "+v"(qf[r]), "+v"(against[r]));
             if (MASK) asm volatile("" : "+v"(q_pos[r]));
-            against[r] = against[r] == -INFINITY ? INFINITY : against[r] * kLog2e;      // (a query that saw nothing gives nothing)
+            used[r] = used[r] & (against[r] != -INFINITY);          // a query that saw nothing gives nothing, whatever it holds
+            against[r] *= kLog2e;
         }
     }
     __device__ __forceinline__ float weights(const bf16x8 (&kf)[4], int32_t kv_pos, float scale_log2) const {
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(kAwWaves * 64, 4) void attn_weights_kernel(WeightsA
             };
             float sum[2][4];
             auto add_columns = [&](float lse, bool used, int32_t q_pos) {
-                const float against = lse == -INFINITY ? INFINITY : lse * kLog2e;   // (a query that saw nothing gives nothing)
+                const float against = lse * kLog2e;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     floatx4 sc = {0.f, 0.f, 0.f, 0.f};
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(kAwWaves * 64, 4) void attn_weights_kernel(WeightsA
                         const float lse = *(const ESP_LDS float*)(uintptr_t)(lds + 4096 + 4 * l16);
                         const int32_t q_pos = MASK ? *(const ESP_LDS int32_t*)(uintptr_t)(lds + 4160 + 4 * l16) : 0;
                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                        const bool used = qb * QB + ql < nq && hb * 16 + hd < G && (G > 16 || l16 < QB * G);
+                        const bool used = qb * QB + ql < nq && hb * 16 + hd < G && (G > 16 || l16 < QB * G) && lse != -INFINITY;   // (a query that saw nothing gives nothing)
                         if (++hb == HB) { hb = 0; ++qb; }
                         if (qb < blocks) bring_chunk(qb, hb);
                         else if (j + 1 < n) bring(j + 1, next);
@@ -433,8 +434,8 @@ __global__ __launch_bounds__((kAwTiles + 1) * 64, 4) void attn_weights_span_kern
                         const float lse = *(const ESP_LDS float*)(uintptr_t)(from + 4096 + 4 * l16);
                         const int32_t q_pos = MASK ? *(const ESP_LDS int32_t*)(uintptr_t)(from + 4160 + 4 * l16) : 0;
                         from = from == lds_chunk + (kAwPlaces - 1) * kChunk ? lds_chunk : from + kChunk;
-                        const float against = lse == -INFINITY ? INFINITY : lse * kLog2e;   // (a query that saw nothing gives nothing)
-                        const bool used = (qb * QB + ql < nq) & (hb * 16 + hd < G) & ((G > 16) | (l16 < QB * G));
+                        const float against = lse * kLog2e;
+                        const bool used = (qb * QB + ql < nq) & (hb * 16 + hd < G) & ((G > 16) | (l16 < QB * G)) & (lse != -INFINITY);   // (a query that saw nothing gives nothing)
                         if (++hb == HB) { hb = 0; ++qb; }
                         floatx4 sc[2];
 #pragma unroll
