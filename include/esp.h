@@ -491,7 +491,8 @@ esp_status esp_build_slots(
  * zeros.  k, v lie on 16 bytes.
  * esp_partial_attn_decode_q4 is esp_partial_attn_decode over such a pool, for any Hq that is a
  * multiple of Hkv.  An infinite value (of those scales) makes the elements of O that it enters infinite.  Weights times
- * values are summed in fp32 before the division, as in all decode calls: over thousands of rows of values next to the largest that sum may pass its range.  q lies on 16 bytes, O on 4.  workspace: at least
+ * values are summed in fp32 before the division, as in all decode calls: over thousands of rows of values next to the largest that sum may pass its range.
+ * softmax_scale * log2(e) is a finite number in this call and the next two (ESP_ERR_INVALID_ARG).  q lies on 16 bytes, O on 4.  workspace: at least
  * esp_decode_q4_workspace_bytes(...) bytes (ESP_ERR_WORKSPACE otherwise), 256-byte aligned; it rises with every size,
  * contents need not be preserved.  Calls that may run at the same time need a workspace each.
  */

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <vector>
 
 #include "attn_weights.h"
@@ -553,6 +554,9 @@ esp_status esp_kv_append(const void* k, const void* v, const int32_t* slot_idx, 
     return launch_kv_append(k, v, slot_idx, T, k_pool, v_pool, Hkv * D * 2, (hipStream_t)stream);
 }
 
+// exponentials are taken to the base 2: with an infinite factor a score of 0 would be NaN
+static bool finite_factor(float softmax_scale) { return std::isfinite(softmax_scale * kLog2e); }
+
 // what the calls on the pool in 4 bits are asked
 static esp_status q4_pool_check(const char* what, const void* k_pool, const void* v_pool, int64_t slot_bytes, int64_t num_slots, int32_t Hkv, int32_t D) {
     if (num_slots < 0 || Hkv <= 0) return fail(ESP_ERR_INVALID_ARG, "%s: negative size", what);
@@ -607,7 +611,7 @@ esp_status esp_partial_attn_decode_q4(const void* q, const void* k_pool, const v
                                       float softmax_scale, void* O, float* LSE, void* workspace, size_t workspace_bytes, void* stream) {
     bool done;
     esp_status st = decode_check(q, k_pool, v_pool, num_slots, slot_idx, seq_offsets, B, total_tokens, max_len, Hq, Hkv, D, softmax_scale, O, LSE, &done);
-    if (st == ESP_OK && softmax_scale > 3e38f) st = fail(ESP_ERR_INVALID_ARG, "decode (4 bits): bad softmax_scale");
+    if (st == ESP_OK && !finite_factor(softmax_scale)) st = fail(ESP_ERR_INVALID_ARG, "decode (4 bits): bad softmax_scale");
     if (st == ESP_OK) st = q4_pool_check("decode (4 bits)", k_pool, v_pool, slot_bytes, num_slots, Hkv, D);
     if (st != ESP_OK || done) return st;
     if ((uintptr_t)q & 15) return fail(ESP_ERR_INVALID_ARG, "decode (4 bits): q is not 16-byte aligned");
@@ -642,7 +646,7 @@ static esp_status weights_entry(const void* q, const float* LSE, const void* k_p
     if (max_q > Tq) return fail(ESP_ERR_INVALID_ARG, "%s: max_q exceeds Tq", what);
     if (!q_offsets && (Tq != B || max_q != (B > 0 ? 1 : 0))) return fail(ESP_ERR_INVALID_ARG, "%s: without q_offsets there is a query to each request", what);
     if ((q_pos == nullptr) != (kv_pos == nullptr)) return fail(ESP_ERR_INVALID_ARG, "%s: q_pos and kv_pos must both be given or both be NULL", what);
-    if (!(softmax_scale >= 0.f) || softmax_scale > 3e38f) return fail(ESP_ERR_INVALID_ARG, "%s: bad softmax_scale", what);
+    if (!(softmax_scale >= 0.f) || !finite_factor(softmax_scale)) return fail(ESP_ERR_INVALID_ARG, "%s: bad softmax_scale", what);
     if (!(decay >= 0.f) || decay > 3e38f) return fail(ESP_ERR_INVALID_ARG, "%s: bad decay", what);
     if (B == 0 || total_tokens == 0) return ESP_OK;
     if (!slot_idx || !seq_offsets || !weight_sum || (Tq > 0 && (!q || !LSE))) return fail(ESP_ERR_INVALID_ARG, "%s: null q/LSE/slot_idx/seq_offsets/weight_sum", what);
