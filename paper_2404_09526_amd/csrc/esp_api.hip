@@ -655,7 +655,7 @@ static esp_status weights_entry(const void* q, const float* LSE, const void* k_p
     if (((uintptr_t)LSE & 3) || ((uintptr_t)weight_sum & 3)) return fail(ESP_ERR_INVALID_ARG, "%s: LSE or weight_sum is not 4-byte aligned", what);
     if (debug_validate()) {
         esp_status st = check_offsets("attention weights: seq_offsets", seq_offsets, B, total_tokens, max_len, (hipStream_t)stream);
-        if (st == ESP_OK && q_offsets) st = check_offsets("attention weights: q_offsets", q_offsets, B, Tq, max_q, (hipStream_t)stream);
+        if (st == ESP_OK && q_offsets) st = check_offsets("attention weights: q_offsets", q_offsets, B, Tq, Tq, (hipStream_t)stream);   // (of more than max_q the first count)
         if (st == ESP_OK) st = check_slots(what, slot_idx, total_tokens, num_slots, false, true, (hipStream_t)stream);
         if (st != ESP_OK) return st;
     }

@@ -1,9 +1,10 @@
-"""Sums of attention weights: queries that saw nothing."""
+"""Sums of attention weights: queries that saw nothing, and requests of more queries than stated."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_evict import check_weights, weights_case
+from paper_2404_09526_amd import binding as esp
+from test_gpu_evict import check_weights, exact_weights, i32, offsets, weights_case
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +27,36 @@ def test_a_query_that_saw_nothing_gives_nothing_whatever_it_holds(cuda, hq, hkv,
     c["q_dev"][torch.from_numpy(nothing).to(cuda)] = float("nan")
     c["q_dev"][0, hq // 2, ::2] = float("inf")
     check_weights(c, decay=0.5, by_offsets=True)
+
+
+def first_queries(c, most):
+    """The case with the first `most` queries of each request alone."""
+    at = offsets(c["queries"])
+    rows = np.concatenate([np.arange(at[b], at[b] + min(most, n)) for b, n in enumerate(c["queries"])]).astype(int)
+    return dict(c, queries=np.minimum(c["queries"], most), q=c["q"][rows], LSE=c["LSE"][rows], q_pos=None if c["q_pos"] is None else c["q_pos"][rows])
+
+
+@pytest.fixture(params=[False, True], ids=["", "validated"])
+def validating(cuda, request):
+    was = esp.esp_debug_set_validate(request.param)
+    yield request.param
+    esp.esp_debug_set_validate(was)
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+@pytest.mark.parametrize("positions", [False, True])
+@pytest.mark.parametrize("hq,hkv,queries,most", [(4, 4, [3, 1, 2], 1), (8, 8, [3, 0, 2], 1), (6, 3, [5, 2, 4], 2), (8, 2, [30, 9, 3], 7), (40, 2, [2, 1, 3], 1), (4, 1, [19, 40, 2], 9)])
+def test_of_more_queries_than_stated_the_first_count(cuda, validating, hq, hkv, queries, most, positions, bits):
+    c = weights_case(cuda, [300, 77, 131], queries, hq, hkv, bits, hq, positions)
+    args = dict(q=c["q_dev"], LSE=torch.from_numpy(c["LSE"]).to(cuda), k_pool=c["pool"], slot_idx=i32(c["slot"], cuda), seq_offsets=i32(offsets(c["lens"]), cuda), max_len=300,
+                weight_sum=torch.from_numpy(c["sums"]).to(cuda), q_offsets=i32(offsets(queries), cuda), max_q=most, q_pos=None if c["q_pos"] is None else i32(c["q_pos"], cuda),
+                kv_pos=None if c["kv_pos"] is None else i32(c["kv_pos"], cuda), decay=0.5, fresh=2)
+    got = esp.esp_accumulate_attn_weights(**args).double().cpu().numpy()
+    want, off = exact_weights(first_queries(c, most), 128 ** -0.5, 0.5, 2)
+    assert (np.abs(got - want) <= off).all()
+    if validating:                                                    # what the checks do refuse: offsets that decrease, or end elsewhere
+        for at, x in ((1, offsets(queries)[2] + 1), (3, sum(queries) - 1), (0, 1)):
+            bad = args["q_offsets"].clone()
+            bad[at] = int(x)
+            with pytest.raises(esp.EspError):
+                esp.esp_accumulate_attn_weights(**dict(args, q_offsets=bad))
