@@ -585,11 +585,9 @@ static Q4Geom q4_geom(int32_t B, int32_t total_tokens, int32_t max_len, int32_t 
     return x;
 }
 
-size_t decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq, int32_t Hkv) {
-    int32_t hw, nt, hgroups;
-    q4_heads(Hkv, hw, nt, hgroups);
-    const int step = nt * kQ4Tile;
-    int64_t ranges = ((int64_t)total_tokens + step - 1) / step;
+// Room for the shortest ranges that any number of KV heads is read in, so that it rises with every size (no range is shorter than two steps of one tile or more).
+size_t decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq) {
+    int64_t ranges = ((int64_t)total_tokens + kQ4Tile - 1) / kQ4Tile;
     if (ranges > kQ4MaxRanges) ranges = kQ4MaxRanges;
     return (size_t)((ranges + 1 + B) * q4_partial_bytes(Hq)) + 256;
 }

@@ -603,7 +603,7 @@ esp_status esp_kv_gather_q4(const void* k_pool, const void* v_pool, int64_t slot
 size_t esp_decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, int32_t D) {
     (void)max_len;
     if (B < 0 || total_tokens < 0 || !decode_heads_supported(Hq, Hkv) || D != kHeadDim) return 0;   // 0: the call would be refused
-    return decode_q4_workspace_bytes(B, total_tokens, Hq, Hkv);
+    return decode_q4_workspace_bytes(B, total_tokens, Hq);
 }
 
 esp_status esp_partial_attn_decode_q4(const void* q, const void* k_pool, const void* v_pool, int64_t slot_bytes, int64_t num_slots, const int32_t* slot_idx,
@@ -616,7 +616,7 @@ esp_status esp_partial_attn_decode_q4(const void* q, const void* k_pool, const v
     if (st != ESP_OK || done) return st;
     if ((uintptr_t)q & 15) return fail(ESP_ERR_INVALID_ARG, "decode (4 bits): q is not 16-byte aligned");
     if (((uintptr_t)O & 3) || ((uintptr_t)LSE & 3)) return fail(ESP_ERR_INVALID_ARG, "decode (4 bits): an output is not 4-byte aligned");
-    const size_t need = decode_q4_workspace_bytes(B, total_tokens, Hq, Hkv);
+    const size_t need = decode_q4_workspace_bytes(B, total_tokens, Hq);
     if (!workspace || workspace_bytes < need)
         return fail(ESP_ERR_WORKSPACE, "decode (4 bits): workspace needs %zu bytes, got %zu", need, workspace ? workspace_bytes : (size_t)0);
     if ((uintptr_t)workspace & 255) return fail(ESP_ERR_WORKSPACE, "decode (4 bits): workspace not 256-byte aligned");

@@ -105,7 +105,7 @@ esp_status launch_kv_append_q4(const void* k, const void* v, int64_t k_stride, i
                                void* v_pool, int64_t slot_bytes, int64_t num_slots, hipStream_t stream);
 esp_status launch_kv_gather_q4(const void* k_pool, const void* v_pool, int64_t slot_bytes, const int32_t* slot_idx, int32_t T, int64_t num_slots, int32_t Hkv,
                                void* k, void* v, hipStream_t stream);
-size_t decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq, int32_t Hkv);
+size_t decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq);
 esp_status launch_decode_q4(const void* q, const void* k_pool, const void* v_pool, int64_t slot_bytes, const int32_t* slot_idx, const int32_t* seq_offsets,
                             int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv, float softmax_scale, void* O, float* LSE,
                             void* workspace, hipStream_t stream);

@@ -18,3 +18,14 @@ def test_a_scale_whose_factor_is_infinite_is_refused(lib, scale):  # noqa: F811
     for call in (lambda s: lib.lib.esp_accumulate_attn_weights(one, one, one, *tail(s)), lambda s: lib.lib.esp_accumulate_attn_weights_q4(one, one, one, 544, *tail(s))):
         assert call(scale) == lib.ESP_ERR_INVALID_ARG and "softmax_scale" in lib.last_error()
         assert call(2.35e38) == lib.ESP_OK
+
+
+def test_the_workspace_of_decode_rises_with_every_size(lib):  # noqa: F811
+    """One that is large enough for a call is so for any with as many requests, entries and heads, or fewer."""
+    rng = random.Random(1)
+    kv = [1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 16, 17, 20, 24, 25, 32, 36, 40]
+    for _ in range(4000):
+        B, T, G, H = int(2 ** rng.uniform(0, 13)), int(2 ** rng.uniform(0, 24)), rng.randint(1, 40), rng.choice(kv)
+        b, t, h = rng.choice([B, rng.randint(0, B)]), rng.choice([T, rng.randint(0, T)]), rng.choice([x for x in kv if x <= H])
+        hq = rng.randint(1, G * H // h) * h
+        assert lib.esp_decode_q4_workspace_bytes(B, T, T, G * H, H, 128) >= lib.esp_decode_q4_workspace_bytes(b, t, t, hq, h, 128) > 0, (B, T, G, H, b, t, hq, h)
