@@ -447,7 +447,10 @@ PyObject* weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
         float scale;
         if (L->sizes() != q->sizes().slice(0, 2) || sums->dim() != 1 || sums->size(0) != p.S || !small(a[5], max_len) || !small(a[13], fresh) || !scale_of(a[11], D, scale) ||
             !PyFloat_CheckExact(a[12])) return nullptr;
-        if (qo ? qo->dim() != 1 || qo->size(0) != B + 1 || !small(a[8], max_q) : a[8] != Py_None || Tq != B) return nullptr;
+        const int32_t one = max_q;                                  // query a request, without offsets
+        if (a[8] != Py_None || qo)
+            if (!small(a[8], max_q)) return nullptr;
+        if (qo ? qo->dim() != 1 || qo->size(0) != B + 1 : max_q != one || Tq != B) return nullptr;
         if (qp && (qp->dim() != 1 || qp->size(0) != Tq || kvp->dim() != 1 || kvp->size(0) != total)) return nullptr;
         const float decay = (float)PyFloat_AS_DOUBLE(a[12]);
         void* s;

@@ -1,10 +1,11 @@
-"""Sums of attention weights: queries that saw nothing, and requests of more queries than stated."""
+"""Sums of attention weights: queries that saw nothing, requests of more queries than stated, and the native argument checks of one query a request."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2404_09526_amd import binding as esp
 from test_gpu_evict import check_weights, exact_weights, i32, offsets, weights_case
+from test_gpu_q4_marshal import calls
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +61,24 @@ def test_of_more_queries_than_stated_the_first_count(cuda, validating, hq, hkv, 
             bad[at] = int(x)
             with pytest.raises(esp.EspError):
                 esp.esp_accumulate_attn_weights(**dict(args, q_offsets=bad))
+
+
+@pytest.mark.parametrize("name", ["weights", "weights_q4"])
+def test_native_checks_take_one_query_a_request_by_name(cuda, monkeypatch, name):
+    """max_q = 1 says what None does."""
+    call, kw, _ = calls(esp, cuda)[name]
+    taken, marshal = [], esp._marshal
+
+    class Spy:
+        def __getattr__(self, what):
+            f = getattr(marshal, what)
+            return lambda *a: (taken.append(f(*a)), taken[-1])[1]
+    monkeypatch.setattr(esp, "_marshal", Spy())
+    sums = []
+    for max_q in (None, 1):
+        kw["weight_sum"].fill_(1)
+        sums.append(call(**(kw | dict(max_q=max_q))).clone())
+    assert taken == [0, 0] and torch.equal(*sums)
+    for bad in (0, 2, -1, 1 << 32):
+        with pytest.raises((ValueError, esp.EspError)):
+            call(**(kw | dict(max_q=bad)))
