@@ -701,7 +701,7 @@ esp_status esp_evict_slots(const float* weight_sum, int64_t num_slots, const int
     const Piece in[] = {{slot_idx, list}, {token_pos, list}, {seq_offsets, offs}, {budgets, (size_t)B * 4}, {weight_sum, (size_t)num_slots * 4}};
     const Piece out[] = {{kept_offsets, offs}, {kept_slots, kept}, {kept_pos, kept}, {freed_offsets, offs}, {freed_slots, (size_t)freed_capacity * 4}};
     auto meet = [](const Piece& x, const Piece& y) {
-        return x.at && y.at && (const char*)x.at < (const char*)y.at + y.bytes && (const char*)y.at < (const char*)x.at + x.bytes;
+        return x.at && y.at && x.bytes && y.bytes && (const char*)x.at < (const char*)y.at + y.bytes && (const char*)y.at < (const char*)x.at + x.bytes;
     };
     for (const Piece& x : out) {
         if ((uintptr_t)x.at & 3) return fail(ESP_ERR_INVALID_ARG, "evict: an output is not 4-byte aligned");

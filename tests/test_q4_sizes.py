@@ -29,3 +29,19 @@ def test_the_workspace_of_decode_rises_with_every_size(lib):  # noqa: F811
         b, t, h = rng.choice([B, rng.randint(0, B)]), rng.choice([T, rng.randint(0, T)]), rng.choice([x for x in kv if x <= H])
         hq = rng.randint(1, G * H // h) * h
         assert lib.esp_decode_q4_workspace_bytes(B, T, T, G * H, H, 128) >= lib.esp_decode_q4_workspace_bytes(b, t, t, hq, h, 128) > 0, (B, T, G, H, b, t, hq, h)
+
+
+def test_lists_without_room_overlap_nothing(lib):  # noqa: F811
+    """A capacity of 0, or no entries, with a pointer into another array."""
+    need = lib.esp_evict_workspace_bytes(3, 100, 60)
+    at = {n: P(1 << (20 + i)) for i, n in enumerate(("sums", "idx", "pos", "off", "ko", "ks", "kp", "fo", "fs", "ws"))}
+
+    def call(S=128, total=100, max_len=60, kc=100, fc=100, **other):
+        a = dict(at, **other)                                         # (a workspace that is too small: refused last, nothing is launched)
+        return lib.lib.esp_evict_slots(a["sums"], S, a["idx"], a["pos"], a["off"], 3, total, max_len, nul, 5, 1, 1, kc, a["ko"], a["ks"], a["kp"], fc, a["fo"], a["fs"], a["ws"],
+                                       need - 1 if total else 1, nul)
+    inside = P((1 << 25) + 200)                                       # of kept_slots
+    for kw in (dict(), dict(fc=0, fs=inside), dict(kc=0, ks=P((1 << 28) + 40), kp=P((1 << 28) + 40)), dict(S=0, sums=inside), dict(total=0, max_len=0, idx=inside, pos=inside)):
+        assert call(**kw) == lib.ESP_ERR_WORKSPACE, kw
+    for kw in (dict(fs=inside), dict(fc=1, fs=inside), dict(S=1, sums=inside), dict(idx=inside), dict(pos=inside)):
+        assert call(**kw) == lib.ESP_ERR_INVALID_ARG and "overlap" in lib.last_error(), kw
