@@ -590,7 +590,6 @@ esp_status launch_attn_weights(WeightsArgs a, bool q4, hipStream_t stream) {
     range = (range + step - 1) / step * step;
     a.range = (int32_t)(range > most ? most : range);
     const int64_t blocks = ((int64_t)a.total_tokens + a.range - 1) / a.range;
-    if (blocks > kWideMost) return fail(ESP_ERR_INVALID_ARG, "attention weights: too many tokens for one launch");
     // Two workgroups to a CU, of up to seven wavefronts with a tile (and one that brings queries: two to a SIMD each; with eight and one a CU had room for one: 164 us for
     // 143000 keys, of five in two even rounds 113, of seven 108).  With fewer tiles a head to a wavefront has more of the chip at
     // work (32 queries, 32 / 8 heads: 8 lists of 4096 or so 38 against 60 us, 16 of them 63 against 73, 64 of 1024 or so 101 against 76, 8 of 16384 150 against 90; 57 queries,

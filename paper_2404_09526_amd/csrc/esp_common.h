@@ -65,9 +65,8 @@ constexpr int kGridX = 1 << 23;
 constexpr int64_t kGridMost = (int64_t)65535 * kGridX;
 inline dim3 row_grid(int64_t blocks) { return dim3((unsigned)(blocks < kGridX ? blocks : kGridX), (unsigned)((blocks + kGridX - 1) / kGridX)); }
 __device__ __forceinline__ int64_t row_block() { return (int64_t)blockIdx.y * kGridX + blockIdx.x; }
-// the same for workgroups of up to 1024 threads (a row of a grid has fewer than 2^32)
+// the same for workgroups of up to 1024 threads (a row of a grid has fewer than 2^32); enough for any number of tokens
 constexpr int kWideX = 1 << 21;
-constexpr int64_t kWideMost = (int64_t)65535 * kWideX;
 inline dim3 wide_grid(int64_t blocks) { return dim3((unsigned)(blocks < kWideX ? blocks : kWideX), (unsigned)((blocks + kWideX - 1) / kWideX)); }
 __device__ __forceinline__ int64_t wide_block() { return (int64_t)blockIdx.y * kWideX + blockIdx.x; }
 

@@ -8,9 +8,6 @@ namespace esp {
 constexpr int kQ4Head = ESP_Q4_HEAD_BYTES;
 constexpr int kQ4Codes = 64;                      // bytes of them that are codes; the scales follow
 
-// heads lie on 4 bytes, no more
-typedef uint32_t u32x4_on4 __attribute__((ext_vector_type(4), aligned(4)));
-
 // The conversions take a scale from the exponent's bits of a float and go by those alone (255: NaN), so a byte of a word of four scales needs no more than to
 // be turned to their place.
 __device__ __forceinline__ float q4_scale(uint32_t scales, int byte) {
