@@ -495,6 +495,8 @@ esp_status esp_build_slots(
  * softmax_scale * log2(e) is a finite number in this call and the next two (ESP_ERR_INVALID_ARG).  q lies on 16 bytes, O on 4.  workspace: at least
  * esp_decode_q4_workspace_bytes(...) bytes (ESP_ERR_WORKSPACE otherwise), 256-byte aligned; it rises with every size,
  * contents need not be preserved.  Calls that may run at the same time need a workspace each.
+ * esp_qk_norm_rope_append and esp_partial_attn_decode_shared take the pool in bf16 alone: rows that the first leaves dense go into this one by
+ * esp_kv_append_q4, and requests that share a prefix have its slots in their own lists.
  */
 #define ESP_Q4_HEAD_BYTES 68
 esp_status esp_kv_append_q4(
@@ -545,8 +547,9 @@ size_t esp_decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t ma
  *   kept_offsets, freed_offsets int32 [B+1]; kept_slots int32 [kept_capacity], kept_pos the same of
  *   token_pos int32 [total_tokens] (NULL: not asked for), freed_slots int32 [freed_capacity].
  *   A list longer than its capacity is cut there, its offsets too; entries past the last stay as they
- *   were.  kept_slots and kept_offsets are a list that the other calls take; freed_slots go back to
- *   the scheduler.  Outputs must not overlap the inputs (ESP_ERR_INVALID_ARG).  B = 0 writes the offsets 0.
+ *   were.  kept_slots and kept_offsets are a list that the other calls take, without room between the requests: to go on
+ *   with it, it becomes the rows of a block table with pages of one token, which esp_extend_block_table (freed_slots are its free
+ *   pages) and esp_build_slots take; larger pages have no holes.  Outputs must not overlap the inputs (ESP_ERR_INVALID_ARG).  B = 0 writes the offsets 0.
  *   workspace: at least esp_evict_workspace_bytes(...) bytes (ESP_ERR_WORKSPACE otherwise), 256-byte
  *   aligned; contents need not be preserved; it rises with every size.
  */

@@ -4,7 +4,8 @@
 //   S^T [32 keys x 16] = K [32 x 128] Q^T [128 x 16],
 // 16 at a time against the tile in registers, and the weights of a key are added over the columns a lane has, the lanes, the heads (of a workgroup, through the
 // LDS; it has all heads of its tokens, so nothing is added by two workgroups and the order is always the same), in fp32.
-// Bound by the memory for one query a request: 256 bytes of a head of a token, or 68; by exponentials from some 16 queries of 4 heads on.
+// Bound by the memory for one query a request: 256 bytes of a head of a token, or 68; for many queries by the waits for their chunks of columns, of which
+// each is little work (32 queries of 4 heads a KV head: vector ALU busy for 30 % of the cycles, matrix cores for 14 %).
 #include "attn_weights.h"
 #include "decode_merge.h"
 #include "mfma_tile.h"
@@ -20,8 +21,9 @@ constexpr int kAwSums = 1792;                     // heads of a workgroup times 
 // The same in all lanes, and to be kept in scalars (the compiler does not read what the kernel might write with scalar loads).
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// What a lane brings of a tile's K rows, and reads of them.  4 bits: lane 5 t + p has piece p of token t (twelve tokens a transfer), the last piece is that which ends with
-// the head; bf16: lane 16 t + p has piece p ^ t % 16 of token t (four a transfer).  Either way the words that 16 tokens' lanes read lie in different banks.
+// What a lane brings of a tile's K rows, and reads of them.  4 bits: lane 5 t + p has piece p of token t (twelve tokens a transfer), the last piece is
+// that which ends with the head; bf16: lane 16 t + p has piece p ^ t % 16 of token t (four a transfer).  Either way the words that 16 tokens' lanes
+// read lie in different banks.
 template <bool Q4>
 struct KTile {
     static constexpr int kPitch = Q4 ? 80 : 256, kTransfers = Q4 ? 3 : 8, kRows = Q4 ? 12 : 4, kBytes = kAwTile * kPitch;
@@ -58,7 +60,8 @@ struct KTile {
             const int32_t slot = Q4 ? sl.s[Q4 ? i : 0] : __shfl(sl.s[0], i * kRows + in_row);
             const uint64_t at = (uint64_t)(uint32_t)slot * slot_bytes + (uint32_t)(Q4 ? within : within ^ ((i & 3) << 6));
             if (!Q4 || in_row < (i < kTransfers - 1 ? kRows : kAwTile - i * kRows)) {
-                // (heads of 68 bytes have lines in common with their neighbours', which stay in the caches; 64 requests of 1024 .. 131072, 6 / 3 heads, 95 us, past them 103)
+                // (heads of 68 bytes have lines in common with their neighbours', which stay in the caches; 64 requests of 1024 .. 131072, 6 / 3 heads,
+                // 95 us, past them 103)
                 if (Q4) load_to_lds_b128_at(lds + i * kRows * kPitch, src + at);
                 else load_to_lds_b128_at_nt(lds + i * kRows * kPitch, src + at);
             }
@@ -101,8 +104,8 @@ __device__ __forceinline__ void add_to_tokens(const float (&sum)[2][4], float* t
     if (l16 < 8 && token < seg) tokens[token] += out;
 }
 
-// One query a request, the other way round: S = Q K^T, so that a lane has keys l16 and l16 + 16 and four of the 16 columns, and little is left to be added across lanes (with
-// a key to 16 lanes half of the instructions of a tile were those).
+// One query a request, the other way round: S = Q K^T, so that a lane has keys l16 and l16 + 16 and four of the 16 columns, and little is left to be
+// added across lanes (with a key to 16 lanes half of the instructions of a tile were those).
 template <bool MASK>
 struct OneQuery {
     bf16x8 qf[4];
@@ -126,8 +129,8 @@ struct OneQuery {
             if (MASK) q_pos[r] = a.q_pos[q0 + (used[r] ? (4 * g + r) / G : 0)];
         }
     }
-    // Waited for here: in the loop that uses them the compiler would wait for them, and for all transfers with them, each time (16 requests of 32 .. 4096, 8 / 8 heads in
-    // bf16, 11.2 against 10.9 us).
+    // Waited for here: in the loop that uses them the compiler would wait for them, and for all transfers with them, each time (16 requests of 32 ..
+    // 4096, 8 / 8 heads in bf16, 11.2 against 10.9 us).
     __device__ __forceinline__ void is_here() {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -267,8 +270,8 @@ __global__ __launch_bounds__(kAwWaves * 64, 4) void attn_weights_kernel(WeightsA
                     if (g % 2 == 0 && token < seg) tokens[token] += both;
                 }
             } else {
-                // Chunks of columns through the LDS, four lanes' 1 KiB each of its 16 rows: operands read from memory by their own lanes kept the address unit busy for
-                // most of the time (32 queries of 4 heads a KV head, 143000 keys, 198 us).
+                // Chunks of columns through the LDS, four lanes' 1 KiB each of its 16 rows: operands read from memory by their own lanes kept the
+                // address unit busy for most of the time (32 queries of 4 heads a KV head, 143000 keys, 198 us).
                 const int blocks = (nq + QB - 1) / QB;
                 const uint32_t query_bytes = (uint32_t)a.Hq * (2 * kHeadDim);
                 // block qb of queries, hb of heads; columns past the last have its query, or head, again
@@ -298,7 +301,8 @@ __global__ __launch_bounds__(kAwWaves * 64, 4) void attn_weights_kernel(WeightsA
                         const float lse = *(const ESP_LDS float*)(uintptr_t)(lds + 4096 + 4 * l16);
                         const int32_t q_pos = MASK ? *(const ESP_LDS int32_t*)(uintptr_t)(lds + 4160 + 4 * l16) : 0;
                         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                        const bool used = qb * QB + ql < nq && hb * 16 + hd < G && (G > 16 || l16 < QB * G) && lse != -INFINITY;   // (a query that saw nothing gives nothing)
+                        // (a query that saw nothing gives nothing)
+                        const bool used = qb * QB + ql < nq && hb * 16 + hd < G && (G > 16 || l16 < QB * G) && lse != -INFINITY;
                         if (++hb == HB) { hb = 0; ++qb; }
                         if (qb < blocks) bring_chunk(qb, hb);
                         else if (j + 1 < n) bring(j + 1, next);
@@ -323,11 +327,12 @@ __global__ __launch_bounds__(kAwWaves * 64, 4) void attn_weights_kernel(WeightsA
     }
 }
 
-// Many queries against long lists: the workgroup's wavefronts have a tile of 32 tokens each and take the heads one after another, so that a chunk of columns is brought
-// once for all of them, and a key's sum stays in registers over all heads.  With a head to a wavefront each brought the queries of its head for every 32 tokens: 32 queries
-// of 4 heads a KV head, 143000 keys, 1.6 GB from the L2, 153 us; so 108.  One wavefront more brings the chunks, three ahead: loads are waited for in their order, and a chunk
-// asked for behind the next head's tile waited for that (156 us, with eight wavefronts at any length).  Meeting once for two chunks, the next two on their way: 125.  Bound by instructions and their latency between two meetings: without
-// its sums 93 us, without memory 120 of then 140.
+// Many queries against long lists: the workgroup's wavefronts have a tile of 32 tokens each and take the heads one after another, so that a chunk of
+// columns is brought once for all of them, and a key's sum stays in registers over all heads.  With a head to a wavefront each brought the queries of
+// its head for every 32 tokens: 32 queries of 4 heads a KV head, 143000 keys, 1.6 GB from the L2, 153 us; so 108.  One wavefront more brings the
+// chunks, three ahead: loads are waited for in their order, and a chunk asked for behind the next head's tile waited for that (156 us, with eight
+// wavefronts at any length).  Meeting once for two chunks, the next two on their way: 125.  Bound by instructions and their latency between two
+// meetings: without its sums 93 us, without memory 120 of then 140.
 constexpr int kAwPlaces = 4;                      // of chunks
 constexpr int kAwTiles = 7;                       // wavefronts with a tile, at most (two workgroups fit a CU)
 template <bool Q4, bool MASK>
@@ -435,7 +440,8 @@ __global__ __launch_bounds__((kAwTiles + 1) * 64, 4) void attn_weights_span_kern
                         const int32_t q_pos = MASK ? *(const ESP_LDS int32_t*)(uintptr_t)(from + 4160 + 4 * l16) : 0;
                         from = from == lds_chunk + (kAwPlaces - 1) * kChunk ? lds_chunk : from + kChunk;
                         const float against = lse * kLog2e;
-                        const bool used = (qb * QB + ql < nq) & (hb * 16 + hd < G) & ((G > 16) | (l16 < QB * G)) & (lse != -INFINITY);   // (a query that saw nothing gives nothing)
+                        // (a query that saw nothing gives nothing)
+                        const bool used = (qb * QB + ql < nq) & (hb * 16 + hd < G) & ((G > 16) | (l16 < QB * G)) & (lse != -INFINITY);
                         if (++hb == HB) { hb = 0; ++qb; }
                         floatx4 sc[2];
 #pragma unroll
@@ -476,10 +482,10 @@ __global__ __launch_bounds__((kAwTiles + 1) * 64, 4) void attn_weights_span_kern
     }
 }
 
-// One query a request against rows of four or eight heads in 4 bits (HW: the workgroup's at a time): K's rows whole, by all wavefronts, as decode reads them.  64 requests of
-// 1024 .. 131072, 32 / 8 heads: 186 us with a line asked for by each head's wavefront, 153 with a key's columns over 16 lanes and the list read again by every step, 127
-// so.  Of these 26 are the sums' own lines, one of 128 bytes for 4; the rows' lines, 5.3 of 128 bytes for 544, come at 5.4 TB/s.  (Two steps on their way, or a
-// workgroup for all tokens of a third of a CU, were no faster: 131.)
+// One query a request against rows of four or eight heads in 4 bits (HW: the workgroup's at a time): K's rows whole, by all wavefronts, as decode reads
+// them.  64 requests of 1024 .. 131072, 32 / 8 heads: 186 us with a line asked for by each head's wavefront, 153 with a key's columns over 16 lanes and
+// the list read again by every step, 127 so.  Of these 26 are the sums' own lines, one of 128 bytes for 4; the rows' lines, 5.3 of 128 bytes for 544,
+// come at 5.4 TB/s.  (Two steps on their way, or a workgroup for all tokens of a third of a CU, were no faster: 131.)
 constexpr int kAwRowsSums = 4096;                 // heads of a workgroup times tokens of its range, at most (three workgroups fit a CU)
 template <int HW>
 __global__ __launch_bounds__(kAwWaves * 64, 6) void attn_weights_rows_kernel(WeightsArgs a) {
@@ -582,6 +588,8 @@ esp_status launch_attn_weights(WeightsArgs a, bool q4, hipStream_t stream) {
     const int64_t tiles = ((int64_t)a.total_tokens + kAwTile - 1) / kAwTile;
     // few tiles: fewer a workgroup, which takes requests one after another (32 queries, 32 / 2 heads, 64 lists of 30 or so, 78 against 32 us)
     a.nt = (int)std::min<int64_t>(kAwWaves / a.hw, (tiles + 511) / 512);
+    // (Whole rows are read where nothing is masked alone: 64 requests of 1024 .. 131072, 32 / 8 heads in 4 bits, 127 us, by positions 178; over other
+    // layouts positions cost little: 6 / 3 heads 93 and 106, 32 / 8 in bf16 333 and 336.)
     const bool by_rows = q4 && !many && !mask && a.Hkv % 4 == 0;
     if (by_rows) { a.hw = a.Hkv % 8 == 0 ? 8 : 4; a.nt = kAwWaves / a.hw; }
     // as many tokens as 512 workgroups get, in steps of the workgroup, no more than there is room for
@@ -590,12 +598,12 @@ esp_status launch_attn_weights(WeightsArgs a, bool q4, hipStream_t stream) {
     range = (range + step - 1) / step * step;
     a.range = (int32_t)(range > most ? most : range);
     const int64_t blocks = ((int64_t)a.total_tokens + a.range - 1) / a.range;
-    // Two workgroups to a CU, of up to seven wavefronts with a tile (and one that brings queries: two to a SIMD each; with eight and one a CU had room for one: 164 us for
-    // 143000 keys, of five in two even rounds 113, of seven 108).  With fewer tiles a head to a wavefront has more of the chip at
-    // work (32 queries, 32 / 8 heads: 8 lists of 4096 or so 38 against 60 us, 16 of them 63 against 73, 64 of 1024 or so 101 against 76, 8 of 16384 150 against 90; 57 queries,
-    // 32 / 4 heads, 147 lists of 282 or so, 136 against 170); lists
-    // that leave most of a workgroup's tiles empty would undo it.  With one KV head there is nothing to lose: 57 queries of 32 heads, 147 lists of 282, 253 against 169
-    // us; 32 queries, 64 lists of 30, 167 against 39; one query, 256 of 50, 23 against 12.
+    // Two workgroups to a CU, of up to seven wavefronts with a tile (and one that brings queries: two to a SIMD each; with eight and one a CU had room
+    // for one: 164 us for 143000 keys, of five in two even rounds 113, of seven 108).  With fewer tiles a head to a wavefront has more of the chip at
+    // work (32 queries, 32 / 8 heads: 8 lists of 4096 or so 38 against 60 us, 16 of them 63 against 73, 64 of 1024 or so 101 against 76, 8 of 16384 150
+    // against 90; 57 queries, 32 / 4 heads, 147 lists of 282 or so, 136 against 170); lists that leave most of a workgroup's tiles empty would undo it.
+    // With one KV head there is nothing to lose: 57 queries of 32 heads, 147 lists of 282, 253 against 169 us; 32 queries, 64 lists of 30, 167 against
+    // 39; one query, 256 of 50, 23 against 12.
     const int64_t each = std::min<int64_t>(kAwTiles, (tiles + 511) / 512);
     if (many && (a.Hkv == 1 || (tiles >= 512 * 4 && tiles * a.Hkv >= 512 * 32 && a.total_tokens / a.B >= 2 * kAwTile * each))) {
         a.nt = (int)each;

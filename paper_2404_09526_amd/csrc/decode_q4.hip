@@ -4,20 +4,21 @@
 // A wavefront has a KV head and tiles of 32 of its tokens; a workgroup has the heads of a whole row (up to eight; fewer heads: several wavefronts to a
 // head, tiles in turn), so a random slot is one burst.  The query heads of the KV head are the columns of the products (16, or NC = 2 times 16):
 //   S^T [32 keys x 16] = K [32 x 128] Q^T [128 x 16],   O^T [128 x 16] += V^T [128 x 32] P^T [32 x 16].
-// Codes and scales go from memory to the LDS by themselves, a step ahead, and where rows are pieces of 16 bytes a row by neighbouring lanes: lanes that each load a row
-// of their own, as the operands have them, kept the address unit busy all the time (97 cycles an instruction; 128 requests of 512 .. 1M tokens, 32 / 8 heads, 1570 us; four
-// lanes to a head of a token 1310, whole rows 645: 3.94 GB of rows at 6.1 TB/s, in 4.19 GB of lines of 128 bytes, 6.6 TB/s.  A second step on its way: 658).
-// Codes become bf16 with their scales on the way from the LDS to the products, exactly.
+// Codes and scales go from memory to the LDS by themselves, a step ahead, and where rows are pieces of 16 bytes a row by neighbouring lanes: lanes that
+// each load a row of their own, as the operands have them, kept the address unit busy all the time (97 cycles an instruction; 128 requests of 512 .. 1M
+// tokens, 32 / 8 heads, 1570 us; four lanes to a head of a token 1310, whole rows 645: 3.94 GB of rows at 6.1 TB/s, in 4.19 GB of lines of 128 bytes,
+// 6.6 TB/s.  A second step on its way: 658).  Codes become bf16 with their scales on the way from the LDS to the products, exactly.
 //   K: a lane has four bytes of each block of a key, eight elements, which are a step of the contraction: operands without a turn.
 //   V: its products need neighbouring keys in a register and codes are neighbours along a key.  A lane takes eight elements of each of eight keys, and
 //   the halves of converted pairs are put together: element 8 c + d of column d of the lanes c makes up the rows of product d.  No turn through the LDS.
 // Values in 4 bits are exact in bf16; the weights are rounded to bf16 for the second product, as in the other decode kernels, and the sum they are
 // divided by is that of the rounded ones.
 //
-// What the weights are taken against follows the scores only when weights get large: any reference serves.  It is set to 2^11 times the largest weight so far, and again
-// when a lane's eight weights pass 1 in sum, which leaves out the maximum of nearly every tile.  No weight is above 1, then, as if each tile's maximum were taken: a row that is
-// much heavier than those before it does not pass the range of fp32, whatever finite values it has.  (Against the largest weight itself, and up to 2048 times it, rows
-// above 2^116 came out infinite.)  What the weights lose at the other end is far below what fp32 and bf16 hold.
+// What the weights are taken against follows the scores only when weights get large: any reference serves.  It is set to 2^11 times the largest weight
+// so far, and again when a lane's eight weights pass 1 in sum, which leaves out the maximum of nearly every tile.  No weight is above 1, then, as if
+// each tile's maximum were taken: a row that is much heavier than those before it does not pass the range of fp32, whatever finite values it has.
+// (Against the largest weight itself, and up to 2048 times it, rows above 2^116 came out infinite.)  What the weights lose at the other end is far
+// below what fp32 and bf16 hold.
 #include <math.h>
 
 #include "decode_merge.h"
@@ -85,8 +86,8 @@ struct Q4Columns {
             }
         }
     }
-    // Of a tile's keys the first `left` count; the ones past them are the last one again.  V's codes (vw as below) become zeros there, as 0 times an infinity, of a scale of
-    // 2^126 or 2^127, is not 0.  (A NaN among its scales shows in the result by the last key itself.)
+    // Of a tile's keys the first `left` count; the ones past them are the last one again.  V's codes (vw as below) become zeros there, as 0 times an
+    // infinity, of a scale of 2^126 or 2^127, is not 0.  (A NaN among its scales shows in the result by the last key itself.)
     static __device__ __forceinline__ void hide(uint32_t (&vw)[2][4], int left, int g) {
         if (left >= kQ4Tile) return;
 #pragma unroll
@@ -169,8 +170,8 @@ struct Q4Columns {
         }
     }
 
-    // The nt wavefronts of a head (this is number tsub; number u's block of 8 KiB is at blocks + (u - 1) * pitch, its row of s_ml u * apart on) combine their results, a
-    // column tile at a time, and one partial leaves for each head, or the result where it is the only one.
+    // The nt wavefronts of a head (this is number tsub; number u's block of 8 KiB is at blocks + (u - 1) * pitch, its row of s_ml u * apart on) combine
+    // their results, a column tile at a time, and one partial leaves for each head, or the result where it is the only one.
     __device__ __forceinline__ void finish(int tsub, int nt, unsigned char* blocks, int pitch, float2 (*s_ml)[16], int apart, int ng, int l16, int g, int lane, bool whole,
                                            int64_t at, float* part_acc, float* part_ml, U32x2* O, float* LSE) {
 #pragma unroll
@@ -241,9 +242,10 @@ struct Q4Columns {
     }
 };
 
-// Range i of those that the requests have, counted from each one's first token on: the whole ones of all requests first, then what is left of each.  A lane looks at
-// K consecutive requests, all at once, then the lanes at those of the lane that has it: two round trips for up to 4096 requests (request_range takes two for each 64,
-// twice over: 64 requests of 1024 .. 131072, 32 / 1 heads, 55 us in ranges along the list, which cross up to four requests).
+// Range i of those that the requests have, counted from each one's first token on: the whole ones of all requests first, then what is left of each.  A
+// lane looks at K consecutive requests, all at once, then the lanes at those of the lane that has it: two round trips for up to 4096 requests
+// (request_range takes two for each 64, twice over: 64 requests of 1024 .. 131072, 32 / 1 heads, 55 us in ranges along the list, which cross up to four
+// requests).
 constexpr int32_t kQ4MostByRequest = 4096;
 __device__ __forceinline__ int32_t wave_scan(int32_t x, int lane) {   // sum up to this lane's
 #pragma unroll
@@ -282,8 +284,8 @@ __device__ __forceinline__ RequestRange q4_request_range(int32_t i, int32_t rang
     return {first + at, t0, t0 + min(range, end - t0), start / range + part};
 }
 
-// A workgroup's way along the token list: what it works on, request after request.  parts == 1: each request whole; > 1: so many ranges of each; < 0: as many as each
-// has; 0: ranges along the list.
+// A workgroup's way along the token list: what it works on, request after request.  parts == 1: each request whole; > 1: so many ranges of each; < 0:
+// as many as each has; 0: ranges along the list.
 struct Q4Walk {
     int b;
     int32_t t0, t1, req_end, w;
@@ -322,10 +324,11 @@ struct Q4Walk {
     __device__ __forceinline__ void done(uint32_t seg) { t0 += (int32_t)seg; ++b; }
 };
 
-// Rows of four or eight heads (HW: the workgroup's), which are pieces of 16 bytes: every wavefront brings whole rows, K's and V's, for all of them, and reads what it needs
-// of the others'.  Nothing is brought past the last step: 64 requests of 32 .. 4096 tokens, 32 / 8 heads, 3 or 4 steps to a workgroup, 22.5 against 23.0 us.
-// Loads go past the caches, but for PART: rows of four heads that are part of a slot's, of which neighbouring workgroups have a good deal of their lines of memory in common
-// (82 requests of 4350 or so, 12 / 12 heads, 210 us, past the caches 220; of eight heads 667 and 662, 32 / 32 heads; whole rows of four 340 and 318, of eight 811 and 755).
+// Rows of four or eight heads (HW: the workgroup's), which are pieces of 16 bytes: every wavefront brings whole rows, K's and V's, for all of them, and
+// reads what it needs of the others'.  Nothing is brought past the last step: 64 requests of 32 .. 4096 tokens, 32 / 8 heads, 3 or 4 steps to a
+// workgroup, 22.5 against 23.0 us.  Loads go past the caches, but for PART: rows of four heads that are part of a slot's, of which neighbouring
+// workgroups have a good deal of their lines of memory in common (82 requests of 4350 or so, 12 / 12 heads, 210 us, past the caches 220; of eight heads
+// 667 and 662, 32 / 32 heads; whole rows of four 340 and 318, of eight 811 and 755).
 template <int HW, int NC, bool PART>
 __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_rows_kernel(
     const uint16_t* __restrict__ q, const char* __restrict__ k_pool, const char* __restrict__ v_pool, const int32_t* __restrict__ slot_idx,
@@ -424,11 +427,12 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_rows
     }
 }
 
-// Any other number of heads, and short requests: every wavefront brings what it needs itself, its head of K and of V of a tile's tokens.  68 bytes are four pieces of 16 and one that ends with
-// them, beside the fourth: five lanes, twelve tokens to a transfer.  A pool of one head that has V next to K (JOINT) has 136 bytes there: nine lanes.  (A line of memory
-// asked for by one instruction and not by several: codes and scales apart were 160 requests a tile, the rate of which bounds such a kernel; these are 98, and 66.)  With NC
-// = 2 there is one workgroup to a CU, and a second tile on its way.  64 requests of 1024 .. 131072, 32 / 1 heads: 43 us, and 5 for the combination; 136 bytes at a random place
-// are two lines of 128 and more, 230 MB, 5.1 TB/s.  The heads' lines overlap, and stay in the caches: 161 requests of 8000 or so, 6 / 3 heads, 258 us, past the caches 332.
+// Any other number of heads, and short requests: every wavefront brings what it needs itself, its head of K and of V of a tile's tokens.  68 bytes are
+// four pieces of 16 and one that ends with them, beside the fourth: five lanes, twelve tokens to a transfer.  A pool of one head that has V next to K
+// (JOINT) has 136 bytes there: nine lanes.  (A line of memory asked for by one instruction and not by several: codes and scales apart were 160 requests
+// a tile, the rate of which bounds such a kernel; these are 98, and 66.)  With NC = 2 there is one workgroup to a CU, and a second tile on its way.  64
+// requests of 1024 .. 131072, 32 / 1 heads: 43 us, and 5 for the combination; 136 bytes at a random place are two lines of 128 and more, 230 MB, 5.1
+// TB/s.  The heads' lines overlap, and stay in the caches: 161 requests of 8000 or so, 6 / 3 heads, 258 us, past the caches 332.
 template <int NC, bool JOINT>
 __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_kernel(
     const uint16_t* __restrict__ q, const char* __restrict__ k_pool, const char* __restrict__ v_pool, const int32_t* __restrict__ slot_idx,
@@ -454,7 +458,8 @@ __global__ __launch_bounds__(kQ4Waves * 64, NC == 1 ? 4 : 2) void decode_q4_kern
     const int64_t from = (int64_t)(active ? head : 0) * kQ4Head + (piece == kPieces - 1 ? kBytes - 16 : 16 * piece);
     const char* const k_src = k_pool + from;
     const char* const v_src = v_pool + from;
-    // on its way out: key l16 (and l16 + 16) for the first product, keys 4 g .. 4 g + 3 (and 16 more) for the second.  The last piece's bytes lie 12 (JOINT: 8) further on.
+    // on its way out: key l16 (and l16 + 16) for the first product, keys 4 g .. 4 g + 3 (and 16 more) for the second.  The last piece's bytes lie 12
+    // (JOINT: 8) further on.
     const uint32_t k_rd = lds + l16 * kPitch + 4 * g, ks_rd = lds + l16 * kPitch + (JOINT ? 64 : 76);
     const uint32_t v_rd = lds + kVRegion + 4 * g * kPitch + (!JOINT ? 4 * l16 : l16 < 15 ? kQ4Head + 4 * l16 : 136), vs_rd = lds + kVRegion + 4 * g * kPitch + (JOINT ? 140 : 76);
 
@@ -538,19 +543,21 @@ static void q4_heads(int32_t Hkv, int32_t& hw, int32_t& nt, int32_t& hgroups) {
     nt = kQ4Waves / hw;
 }
 
-// Ranges of the token list, along it or counted from each request's first token on: as many as fill 1 .. 8 rounds of the workgroups that are on the chip at once, none
-// of less than two steps, whichever is estimated to take the least time.  A round is a start and an end, and the steps.  Along the list some workgroup has a start and an
-// end more, 8 us, for a request that its range crosses into, which the others' longer work hides; by request there are some B / 2 ranges more, and the others longer (64 requests
-// of 1024 .. 131072, 32 / 1 heads, 64 us along the list, 49 by request).  Where no request has more ranges than are on the chip at once for all, each gets so many without a
-// search, and a request that is no longer than a range is one workgroup's, which writes the result itself.
+// Ranges of the token list, along it or counted from each request's first token on: as many as fill 1 .. 8 rounds of the workgroups that are on the
+// chip at once, none of less than two steps, whichever is estimated to take the least time.  A round is a start and an end, and the steps.  Along the
+// list some workgroup has a start and an end more, 8 us, for a request that its range crosses into, which the others' longer work hides; by request
+// there are some B / 2 ranges more, and the others longer (64 requests of 1024 .. 131072, 32 / 1 heads, 64 us along the list, 49 by request).  Where no
+// request has more ranges than are on the chip at once for all, each gets so many without a search, and a request that is no longer than a range is one
+// workgroup's, which writes the result itself.
 static Q4Geom q4_geom(int32_t B, int32_t total_tokens, int32_t max_len, int32_t Hq, int32_t Hkv) {
     Q4Geom x;
     const int G = Hq / Hkv;
     q4_heads(Hkv, x.hw, x.nt, x.hgroups);
     x.tiles = G > 16 ? 2 : 1;
     x.chunks = (G + 16 * x.tiles - 1) / (16 * x.tiles);
-    // Short requests, few enough that each KV head of each can have a workgroup of its own: a tile to each wavefront at a time, and no second launch (32 / 8 heads: 4 of up to
-    // 1024 tokens 10.6 against 8.6 us, 64 of 512 19.1 against 12.9, 64 of 1024 24.1 against 20.9; one of 2048 is better in ranges, 10.5 against 13.8).
+    // Short requests, few enough that each KV head of each can have a workgroup of its own: a tile to each wavefront at a time, and no second launch
+    // (32 / 8 heads: 4 of up to 1024 tokens 10.6 against 8.6 us, 64 of 512 19.1 against 12.9, 64 of 1024 24.1 against 20.9; one of 2048 is better in
+    // ranges, 10.5 against 13.8).
     if (max_len <= 1024 && (int64_t)B * Hkv * x.chunks <= (x.tiles == 1 ? 512 : 256)) {
         x.hw = 1;
         x.nt = max_len > (kQ4Waves - 1) * kQ4Tile ? kQ4Waves : max_len > 0 ? (max_len + kQ4Tile - 1) / kQ4Tile : 1;
@@ -585,7 +592,8 @@ static Q4Geom q4_geom(int32_t B, int32_t total_tokens, int32_t max_len, int32_t 
     return x;
 }
 
-// Room for the shortest ranges that any number of KV heads is read in, so that it rises with every size (no range is shorter than two steps of one tile or more).
+// Room for the shortest ranges that any number of KV heads is read in, so that it rises with every size (no range is shorter than two steps of one tile
+// or more).
 size_t decode_q4_workspace_bytes(int32_t B, int32_t total_tokens, int32_t Hq) {
     int64_t ranges = ((int64_t)total_tokens + kQ4Tile - 1) / kQ4Tile;
     if (ranges > kQ4MaxRanges) ranges = kQ4MaxRanges;

@@ -1,17 +1,17 @@
 // esp_evict_slots: of each request's list the entries that stay: its first ones, its last ones, and of the others those with the largest sums (of
-// attention weights), up to a budget; both lists keep the order that the entries had.  Four bytes of a list entry and four of its slot's sum are read, four written: what
-// counts is the number of steps that depend on each other.
+// attention weights), up to a budget; both lists keep the order that the entries had.  Four bytes of a list entry and four of its slot's sum are read,
+// four written: what counts is the number of steps that depend on each other.
 //
-// The smallest sum that stays is found by its digits, from the highest on: sums as unsigned numbers that order alike, 11, 11 and 10 bits, a histogram of the digit among the
-// entries that have the digits found so far, and the digit in which the count of larger ones passes what is to be kept.  Of entries equal to it the first ones stay.
-// Counts are whole numbers: the order in which they are added does not matter.
+// The smallest sum that stays is found by its digits, from the highest on: sums as unsigned numbers that order alike, 11, 11 and 10 bits, a histogram
+// of the digit among the entries that have the digits found so far, and the digit in which the count of larger ones passes what is to be kept.  Of
+// entries equal to it the first ones stay.  Counts are whole numbers: the order in which they are added does not matter.
 //   Where no list is longer than 2048 entries each is one workgroup's: entries in its registers, histograms in its LDS, one launch.
-//   Otherwise a first launch takes the sums of all entries, a lane's each from another line of memory: a CU is given some 0.15 lines a cycle, so 16384 entries that
-//   one CU took for itself were 44 us, spread over all of them 3.  Lists of up to 16384 are one workgroup's again: 16 lists of 32 .. 4096 2.7 and 7.3 us, most of it three
-//   times a histogram, a search and a wait; 162 of 45 .. 11760 21 us, in chunks 27, 4 of 16000 24 and 25.
-//   Where one is longer, those of more than 4096 are cut into chunks of 4096: each digit is a launch over all of them, with a histogram per request in the workspace; with the last one a chunk leaves what it
-//   would keep for each last digit, so that the next launch can write its part behind those before it.  64 lists of 1024 .. 131072: sums 9.6 us, digits 5.2, 5.4 and 6.2,
-//   lists 9.8.
+//   Otherwise a first launch takes the sums of all entries, a lane's each from another line of memory: a CU is given some 0.15 lines a cycle, so 16384
+//   entries that one CU took for itself were 44 us, spread over all of them 3.  Lists of up to 16384 are one workgroup's again: 16 lists of 32 .. 4096
+//   2.7 and 7.3 us, most of it three times a histogram, a search and a wait; 162 of 45 .. 11760 21 us, in chunks 27, 4 of 16000 24 and 25.
+//   Where one is longer, those of more than 4096 are cut into chunks of 4096: each digit is a launch over all of them, with a histogram per request in
+//   the workspace; with the last one a chunk leaves what it would keep for each last digit, so that the next launch can write its part behind those
+//   before it.  64 lists of 1024 .. 131072: sums 9.6 us, digits 5.2, 5.4 and 6.2, lists 9.8.
 #include "evict.h"
 
 namespace esp {
@@ -24,9 +24,9 @@ constexpr int kEvMiddle = 16 * kEvThreads;        // the same, where none is lon
 constexpr int kEvChunk = kEvRounds * kEvThreads;  // of the longer ones
 constexpr int kEvBins = 2048, kEvHist = 2 * kEvBins + 1024;   // of a digit at most; of the three digits
 constexpr int kEvFrom = 1025 + 7;                 // (a multiple of 16 bytes)
-// Requests up to which a workgroup adds up those before its own by itself, in one launch.  That work goes by their square, and is still the less of the two: 1024 lists of
-// 4 .. 64 8.3 us, by the two launches for longer lists 17.1; 8192 of 1 .. 64 54 against 92, of 64 .. 1024 89 against 169; past it 16384 of 1 .. 64 156 against 181, 24576
-// 314 against 277.
+// Requests up to which a workgroup adds up those before its own by itself, in one launch.  That work goes by their square, and is still the less of the
+// two: 1024 lists of 4 .. 64 8.3 us, by the two launches for longer lists 17.1; 8192 of 1 .. 64 54 against 92, of 64 .. 1024 89 against 169; past it
+// 16384 of 1 .. 64 156 against 181, 24576 314 against 277.
 constexpr int32_t kEvOwnOffsets = 8192;
 
 // where the launches for long lists keep what they share
@@ -98,8 +98,9 @@ __device__ __forceinline__ int32_t before(int32_t x, int32_t& all, int32_t* s_wa
     return (wave > 0 ? __shfl(w, wave - 1) : 0) + upto - x;
 }
 
-// The digit in which the count of entries, from the highest digit on, passes `want` (at least 1, at most the histogram's sum), how many of its entries are still to be taken,
-// and whether those are all that it has.  By one wavefront: a lane has BINS / 64 digits in a row.  Digit d's count lies at place(d), so that lanes read different banks.
+// The digit in which the count of entries, from the highest digit on, passes `want` (at least 1, at most the histogram's sum), how many of its entries
+// are still to be taken, and whether those are all that it has.  By one wavefront: a lane has BINS / 64 digits in a row.  Digit d's count lies at
+// place(d), so that lanes read different banks.
 template <int BINS> __device__ __forceinline__ int place(uint32_t d) { return (int)((d & (BINS / 64 - 1)) * 64 + d / (BINS / 64)); }
 struct Digit { uint32_t digit; int32_t want, all; };
 template <int BINS, class P>
@@ -132,8 +133,8 @@ struct EvictShared {
     Digit digit[3];
 };
 
-// Entries with a flag before this one's, in the order of i = threads * j + thread (J rounds, flags[j] the round's flags of this wavefront): the table's entry for (j,
-// wavefront) plus the wavefront's own before the lane.
+// Entries with a flag before this one's, in the order of i = threads * j + thread (J rounds, flags[j] the round's flags of this wavefront): the table's
+// entry for (j, wavefront) plus the wavefront's own before the lane.
 template <int WAVES, int J>
 __device__ __forceinline__ void count_flags(const uint64_t (&flags)[J], int32_t* table) {
     constexpr int N = (J * WAVES + 63) / 64;                        // entries of a lane, in a row
@@ -171,8 +172,8 @@ __device__ __forceinline__ void put(const EvictArgs& a, bool keep, int64_t kept_
     }
 }
 
-// A request of up to J entries for each of the workgroup's threads.  Without keys: they are taken here, and the places of its lists added up (and written); otherwise both
-// are there.
+// A request of up to J entries for each of the workgroup's threads.  Without keys: they are taken here, and the places of its lists added up (and
+// written); otherwise both are there.
 template <int THREADS, int J>
 __device__ void evict_one(const EvictArgs& a, int32_t b, const uint32_t* keys, EvictShared<THREADS / 64, J>& s) {
     constexpr int WAVES = THREADS / 64;
@@ -372,7 +373,8 @@ __global__ __launch_bounds__(kEvThreads) void evict_digit_kernel(EvictArgs a, Ev
     }
 }
 
-// Then each chunk writes what stays of it behind what stays of those before it.  This launch, which takes longest by itself, also has the short lists, in its first workgroups.
+// Then each chunk writes what stays of it behind what stays of those before it.  This launch, which takes longest by itself, also has the short lists,
+// in its first workgroups.
 __global__ __launch_bounds__(kEvThreads, 8) void evict_chunk_kernel(EvictArgs a, EvictSpace w, int32_t chunks) {
     constexpr int J = kEvRounds, WAVES = kEvThreads / 64;
     __shared__ EvictShared<WAVES, kEvRounds> s;

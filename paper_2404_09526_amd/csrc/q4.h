@@ -23,7 +23,8 @@ __device__ __forceinline__ uint4 q4_to_bf16(uint32_t codes, float scale) {
 }
 
 // A block's scale from its largest magnitude, as a bf16 pattern: the power of two with which no element is off by more than half a step (up to 7 of them
-// round to the largest code's 6; from there on, the next one; at most 2^125, with which all codes are finite numbers).  A block with an infinity or a NaN is NaN.
+// round to the largest code's 6; from there on, the next one; at most 2^125, with which all codes are finite numbers).  A block with an infinity or a
+// NaN is NaN.
 __device__ __forceinline__ uint32_t q4_scale_byte(uint32_t largest) {
     const int e = (int)((largest + 0x20) >> 7) - 2;
     return largest >= 0x7f80 ? 255u : (uint32_t)min(max(e, 2), 252);

@@ -1,6 +1,6 @@
 // esp_kv_append_q4, esp_kv_gather_q4: rows on their way into and out of the pool in 4 bits.  Bound by the memory: a head is 256 bytes dense
-// and 68 in the pool.  16 lanes have a head of K and of V, 8 elements each: a block of 32 is four neighbouring lanes.  32768 rows of 8 heads, a quarter of them kept, in 13 us,
-// 65536 rows back in 49: 6.2 TB/s read and written (a copy of 4 GiB: 4.8).
+// and 68 in the pool.  16 lanes have a head of K and of V, 8 elements each: a block of 32 is four neighbouring lanes.  32768 rows of 8 heads, a quarter
+// of them kept, in 13 us, 65536 rows back in 49: 6.2 TB/s read and written (a copy of 4 GiB: 4.8).
 #include "q4.h"
 
 namespace esp {
